@@ -1,4 +1,4 @@
-"""ctypes binding of libdycl.so: the same names as include/dycl.h.
+"""ctypes binding of libdycl.so: the same names as the headers under include/.
 
 Argument marshalling only.  The library is loaded from this package's
 directory; if it is missing, importing the binding raises at once (there is
@@ -23,6 +23,9 @@ EXPORTS = ["dycl_plan_create", "dycl_run", "dycl_run_seq", "dycl_plan_set_host_m
 OPS_EXPORTS = ["dycl_op_compact_workspace", "dycl_op_compact", "dycl_op_compact_noalloc", "dycl_op_move_rows", "dycl_op_conv_packed_bytes",
                "dycl_op_conv_pack", "dycl_op_conv_workspace_bytes", "dycl_op_conv", "dycl_op_conv_maxpool",
                "dycl_op_conv_pair"]
+# every symbol include/dycl_tokens.h declares
+TOKENS_EXPORTS = ["dycl_op_norm", "dycl_op_route_workspace", "dycl_op_route", "dycl_op_linear_packed_bytes", "dycl_op_linear_pack",
+                  "dycl_op_linear_workspace", "dycl_op_linear", "dycl_op_experts_workspace", "dycl_op_experts"]
 
 
 class DyclError(RuntimeError):
@@ -94,6 +97,27 @@ def _load():
     lib.dycl_op_conv_maxpool.restype = i32
     lib.dycl_op_conv_pair.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp]
     lib.dycl_op_conv_pair.restype = i32
+    i64, sz, f32 = C.c_int64, C.c_size_t, C.c_float
+    lib.dycl_op_norm.argtypes = [vp, i32, i64, vp, i32, i64, vp, i64, i32, vp, vp, f32, i32, vp, vp, i32, vp, vp, f32, i64, i32,
+                                 vp, i64, vp, i32, i64, vp]
+    lib.dycl_op_norm.restype = i32
+    lib.dycl_op_route_workspace.argtypes = [i64, i32, i32]
+    lib.dycl_op_route_workspace.restype = sz
+    lib.dycl_op_route.argtypes = [vp, i32, i64, vp, vp, i64, i32, i32, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dycl_op_route.restype = i32
+    lib.dycl_op_linear_packed_bytes.argtypes = [i32, i32, i32, i32]
+    lib.dycl_op_linear_packed_bytes.restype = sz
+    lib.dycl_op_linear_pack.argtypes = [vp, vp, i32, i32, i32, vp, sz, vp]
+    lib.dycl_op_linear_pack.restype = i32
+    lib.dycl_op_linear_workspace.argtypes = [vp, i64, i64, i32, i32, i32]
+    lib.dycl_op_linear_workspace.restype = sz
+    lib.dycl_op_linear.argtypes = [vp, i64, i64, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i32, i64, vp, sz, vp]
+    lib.dycl_op_linear.restype = i32
+    lib.dycl_op_experts_workspace.argtypes = [vp, i64, i64, i32, i32, i32, i32]
+    lib.dycl_op_experts_workspace.restype = sz
+    lib.dycl_op_experts.argtypes = [vp, i64, i64, i32, i32, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp,
+                                    i64, vp, sz, vp]
+    lib.dycl_op_experts.restype = i32
     return lib
 
 

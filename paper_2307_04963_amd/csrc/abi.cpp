@@ -2,12 +2,12 @@
 // Nothing thrown inside the library crosses this boundary.
 #include <algorithm>
 #include <cstring>
-#include <new>
 #include <string>
 
+#include "abi.hpp"
 #include "plan.hpp"
 
-namespace {
+namespace dycl {
 
 thread_local std::string g_err;
 
@@ -16,31 +16,18 @@ int fail(int code, const std::string& msg) {
   return code;
 }
 
+}  // namespace dycl
+
+namespace {
+
+using dycl::fail;
+using dycl::g_err;
+using dycl::guarded;
+
 bool valid(const dycl_plan* p) { return p != nullptr && p->magic == 0x44594350u; }
 
 const char* kClassNames[dycl::P_COUNT] = {"conv_bf16_mfma", "linear_f32", "decision_heads", "compaction",
                                           "gather_scatter", "maxpool", "misc"};
-
-template <class F>
-int guarded(F&& f) {
-  try {
-    return f();
-  } catch (const dycl::WeightsError& e) {
-    return fail(DYCL_E_WEIGHTS, e.what());
-  } catch (const dycl::SpecError& e) {
-    return fail(DYCL_E_SPEC, e.what());
-  } catch (const dycl::OomError& e) {
-    return fail(DYCL_E_OOM, e.what());
-  } catch (const dycl::HipError& e) {
-    return fail(DYCL_E_HIP, e.what());
-  } catch (const std::bad_alloc&) {
-    return fail(DYCL_E_OOM, "host allocation failed");
-  } catch (const std::exception& e) {
-    return fail(DYCL_E_INVALID, e.what());
-  } catch (...) {
-    return fail(DYCL_E_INVALID, "unknown failure");
-  }
-}
 
 }  // namespace
 

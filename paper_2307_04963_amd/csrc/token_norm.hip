@@ -1,0 +1,301 @@
+// The norm after a block, its gate, the residual sum and the norm before the
+// next block in one pass:
+//   z = post(y) * act(gate) * channel_scale * row_gate;  h = a x + z;  u = pre(h)
+// Bound by HBM: x, y and the gate are read once, h and u written once.  T
+// lanes hold a row in registers, so both norms' statistics (float32; the
+// layer norm's variance from the centred values) come from one read.  A
+// workgroup walks over rows with the weights in registers (read for every
+// row they would double the loads), and requests the next row before it
+// reduces the present one.
+#include "token_dev.hpp"
+
+namespace dycl {
+namespace k {
+
+namespace {
+
+// 8 elements of a row, as loaded
+template <bool F32>
+struct Raw {
+  uint4 v[F32 ? 2 : 1];
+};
+
+// VEC: 8 consecutive elements from `i0`, all inside the row or none; else
+// elements i0 + j * T, each checked
+template <bool F32, bool VEC, int T>
+__device__ __forceinline__ Raw<F32> load8(const void* row, int i0, int d) {
+  Raw<F32> r;
+  if constexpr (VEC) {
+#pragma unroll
+    for (int q = 0; q < (F32 ? 2 : 1); ++q) r.v[q] = make_uint4(0, 0, 0, 0);
+    if (i0 < d) {
+      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + static_cast<size_t>(i0) * (F32 ? 4 : 2));
+#pragma unroll
+      for (int q = 0; q < (F32 ? 2 : 1); ++q) r.v[q] = p[q];
+    }
+  } else {
+    uint32_t e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * T;
+      e[j] = 0;
+      if (i < d) e[j] = F32 ? static_cast<const uint32_t*>(row)[i] : static_cast<const uint16_t*>(row)[i];
+    }
+    if constexpr (F32) {
+      r.v[0] = make_uint4(e[0], e[1], e[2], e[3]);
+      r.v[1] = make_uint4(e[4], e[5], e[6], e[7]);
+    } else {
+      r.v[0] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    }
+  }
+  return r;
+}
+
+template <bool F32>
+__device__ __forceinline__ void unpack8(const Raw<F32>& r, float* f) {
+  if constexpr (F32) {
+    const uint32_t e[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(e[j]);
+  } else {
+    const uint32_t e[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f[2 * j] = __uint_as_float(e[j] << 16);
+      f[2 * j + 1] = __uint_as_float(e[j] & 0xffff0000u);
+    }
+  }
+}
+
+template <bool VEC, int T>
+__device__ __forceinline__ void store8(void* row, bool f32, int i0, int d, const float* f) {
+  if constexpr (VEC) {
+    if (i0 >= d) return;
+    if (f32) {
+      float4* p = reinterpret_cast<float4*>(static_cast<float*>(row) + i0);
+      p[0] = make_float4(f[0], f[1], f[2], f[3]);
+      p[1] = make_float4(f[4], f[5], f[6], f[7]);
+    } else {
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + i0) =
+          make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * T;
+      if (i >= d) continue;
+      if (f32)
+        static_cast<float*>(row)[i] = f[j];
+      else
+        static_cast<uint16_t*>(row)[i] = f2bf(f[j]);
+    }
+  }
+}
+
+// the sum over the T lanes of a row; `slot` is this reduction's own LDS
+template <int T>
+__device__ __forceinline__ float row_sum(float v, float* slot) {
+  v = wave_sum(v);
+  if constexpr (T > 64) {
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) v += slot[w];
+  }
+  return v;
+}
+
+template <int T, int NV, bool VEC, bool XF, bool YF, bool BIAS>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void token_norm_kernel(NormArgs p) {
+  constexpr int ROWS = T < 256 ? 256 / T : 1;
+  // a reduction's slot is written again two rows later at the earliest, with
+  // a barrier of the row between
+  __shared__ float slots[2][4][T > 64 ? T / 64 : 1];
+  const int t = threadIdx.x % T;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / T;
+  const int d = p.d;
+  auto at = [&](int i) { return VEC ? (i * T + t) * 8 : i * 8 * T + t; };
+  auto in = [&](int i, int j) { return VEC ? at(i) < d : at(i) + j * T < d; };
+
+  // post's weight and bias with the channel's scale, pre's weight and bias
+  float pw[NV][8], pb[NV][8], qw[NV][8], qb[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int c = VEC ? at(i) + j : at(i) + j * T;
+      const bool ok = in(i, j);
+      const float s = ok && p.channel_scale ? p.channel_scale[c] : 1.f;
+      pw[i][j] = s * (ok && p.post_w ? p.post_w[c] : 1.f);
+      qw[i][j] = ok && p.pre_w ? p.pre_w[c] : 1.f;
+      if (BIAS) {
+        pb[i][j] = s * (ok && p.post_b ? p.post_b[c] : 0.f);
+        qb[i][j] = ok && p.pre_b ? p.pre_b[c] : 0.f;
+      }
+    }
+
+  const float inv_d = 1.0f / static_cast<float>(d);
+  Raw<XF> xr[NV];
+  Raw<YF> yr[NV];
+  float rg = 1.f;
+  auto request = [&](int64_t row) {
+    rg = p.row_gate ? p.row_gate[row] : 1.f;
+    const char* xp = static_cast<const char*>(p.x) + row * p.ldx * (XF ? 4 : 2);
+    const char* yp = static_cast<const char*>(p.y) + row * p.ldy * (YF ? 4 : 2);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) xr[i] = load8<XF, VEC, T>(xp, at(i), d);
+    if (p.y && rg != 0.f) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) yr[i] = load8<YF, VEC, T>(yp, at(i), d);
+    }
+  };
+
+  if (first >= p.n) return;
+  request(first);
+  int parity = 0;
+  // (T > 64: a row per workgroup, so every lane takes the same turns)
+  for (int64_t row = first; row < p.n; row += step, parity ^= 1) {
+    float h[NV][8], z[NV][8];
+    const float gate_of_row = rg;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      unpack8<XF>(xr[i], h[i]);
+      unpack8<YF>(yr[i], z[i]);
+    }
+    if (row + step < p.n) request(row + step);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[i][j] *= p.residual_scale;
+
+    // (a skipped row takes its turn in the reductions, of zeros)
+    if (p.y) {
+      if (gate_of_row == 0.f) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[i][j] = 0.f;
+      }
+      float mean = 0.f, inv = 1.f;
+      if (p.post == 2) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s += z[i][j];
+        mean = row_sum<T>(s, slots[parity][0]) * inv_d;
+      }
+      if (p.post != 0) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float c = in(i, j) ? z[i][j] - mean : 0.f;
+            s = fmaf(c, c, s);
+          }
+        inv = rsqrtf(row_sum<T>(s, slots[parity][1]) * inv_d + p.eps);
+      }
+      if (gate_of_row != 0.f) {
+        const char* gp = static_cast<const char*>(p.gate) + row * p.ldg * (YF ? 4 : 2);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float g[8];
+          if (p.gate) unpack8<YF>(load8<YF, VEC, T>(gp, at(i), d), g);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float v = (z[i][j] - mean) * inv;
+            v = BIAS ? fmaf(v, pw[i][j], pb[i][j]) : v * pw[i][j];
+            if (p.gate) v *= p.gate_act == 0 ? g[j] : (p.gate_act == 1 ? 1.f : g[j]) * sigmoid_fast(g[j]);
+            h[i][j] = fmaf(v, gate_of_row, h[i][j]);
+          }
+        }
+      }
+    }
+    if (p.h) {
+      char* hp = static_cast<char*>(p.h) + row * p.ldh * (XF ? 4 : 2);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) store8<VEC, T>(hp, XF, at(i), d, h[i]);
+    }
+    if (p.u) {
+      float mean = 0.f, inv = 1.f;
+      if (p.pre == 2) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s += in(i, j) ? h[i][j] : 0.f;
+        mean = row_sum<T>(s, slots[parity][2]) * inv_d;
+      }
+      if (p.pre != 0) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float c = in(i, j) ? h[i][j] - mean : 0.f;
+            s = fmaf(c, c, s);
+          }
+        inv = rsqrtf(row_sum<T>(s, slots[parity][3]) * inv_d + p.eps);
+      }
+      char* up = static_cast<char*>(p.u) + row * p.ldu * (p.u_f32 ? 4 : 2);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float c = (h[i][j] - mean) * inv;
+          v[j] = BIAS ? fmaf(c, qw[i][j], qb[i][j]) : c * qw[i][j];
+        }
+        store8<VEC, T>(up, p.u_f32, at(i), d, v);
+      }
+    }
+  }
+}
+
+template <int T, int NV, bool VEC, bool XF, bool YF>
+void launch(const NormArgs& a, hipStream_t s) {
+  constexpr int NT = T < 256 ? 256 : T, ROWS = T < 256 ? 256 / T : 1;
+  const int64_t blocks = (a.n + ROWS - 1) / ROWS;
+  const int most = 256 * (T == 1024 ? 2 : 6);
+  const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
+  if (a.post_b || a.pre_b)
+    token_norm_kernel<T, NV, VEC, XF, YF, true><<<grid, NT, 0, s>>>(a);
+  else
+    token_norm_kernel<T, NV, VEC, XF, YF, false><<<grid, NT, 0, s>>>(a);
+}
+
+template <int T, int NV, bool VEC>
+void by_type(const NormArgs& a, hipStream_t s) {
+  if (a.x_f32)
+    a.y_f32 ? launch<T, NV, VEC, true, true>(a, s) : launch<T, NV, VEC, true, false>(a, s);
+  else
+    a.y_f32 ? launch<T, NV, VEC, false, true>(a, s) : launch<T, NV, VEC, false, false>(a, s);
+}
+
+template <bool VEC>
+void by_size(const NormArgs& a, hipStream_t s) {
+  if (a.d <= 512) return by_type<64, 1, VEC>(a, s);
+  if (a.d <= 1024) return by_type<64, 2, VEC>(a, s);
+  if (a.d <= 2048) return by_type<256, 1, VEC>(a, s);
+  if (a.d <= 4096) return by_type<256, 2, VEC>(a, s);
+  if (a.d <= 8192) return by_type<256, 4, VEC>(a, s);
+  if (a.d <= 16384) return by_type<1024, 2, VEC>(a, s);
+  by_type<1024, 4, VEC>(a, s);
+}
+
+}  // namespace
+
+void token_norm(const NormArgs& a, hipStream_t s) {
+  auto aligned = [](const void* q, int64_t ld, bool f32) {
+    return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * (f32 ? 4 : 2) % 16 == 0);
+  };
+  const bool vec = a.d % 8 == 0 && aligned(a.x, a.ldx, a.x_f32) && aligned(a.y, a.ldy, a.y_f32) &&
+                   aligned(a.gate, a.ldg, a.y_f32) && aligned(a.h, a.ldh, a.x_f32) && aligned(a.u, a.ldu, a.u_f32);
+  vec ? by_size<true>(a, s) : by_size<false>(a, s);
+}
+
+}  // namespace k
+}  // namespace dycl
