@@ -65,6 +65,9 @@ __global__ __launch_bounds__(256) void token_align_kernel(const uint16_t* x, int
 
 // ---- tiles ---------------------------------------------------------------------
 
+// the same value in every lane, in a scalar register
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Rows [row0, row0 + rows) of the product, all of one layer.
 struct Tile {
   int expert;
@@ -98,16 +101,49 @@ __device__ __forceinline__ bool find_tile(const ProductArgs& p, int bm, int64_t 
     const uint64_t found = __ballot(t < before + incl);
     if (found) {
       const int from = __ffsll(static_cast<unsigned long long>(found)) - 1;
-      const int in = static_cast<int>(t - before) - (__shfl(incl, from) - __shfl(tiles, from));
-      const int first = __shfl(lo, from) + in * bm, end = __shfl(hi, from);
+      const int in = static_cast<int>(t - before) - uniform(__shfl(incl, from) - __shfl(tiles, from));
+      const int first = uniform(__shfl(lo, from)) + in * bm, end = uniform(__shfl(hi, from));
       out.expert = e0 + from;
       out.row0 = first;
       out.rows = end - first < bm ? end - first : bm;
       return true;
     }
-    before += __shfl(incl, 63);
+    before += uniform(__shfl(incl, 63));
   }
   return false;
+}
+
+// The tile of this workgroup: row tile and column tile.  Workgroups are dealt
+// round-robin over the 8 XCDs, so each XCD takes a contiguous range of the
+// tiles, in which runs of kGroup row tiles go over the columns together: 32
+// workgroups that are resident at a time share 8 row tiles and 4 column tiles
+// in their XCD's L2.
+constexpr int kGroup = 8;
+
+__device__ __forceinline__ bool tile_of(const ProductArgs& p, int bm, int col_tiles, Tile& out, int& col) {
+  int64_t row_tiles = (p.rows + bm - 1) / bm;
+  if (p.offsets) {
+    row_tiles = 0;
+    const int lane = threadIdx.x & 63;
+    for (int e0 = 0; e0 < p.experts; e0 += 64) {
+      const int e = e0 + lane;
+      const int rows = e < p.experts ? p.offsets[e + 1] - p.offsets[e] : 0;
+      int tiles = (rows + bm - 1) / bm;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) tiles += __shfl_xor(tiles, o);
+      row_tiles += uniform(tiles);
+    }
+  }
+  const int64_t all = row_tiles * col_tiles, each = all >> 3;
+  const int64_t wg = blockIdx.x;
+  if (wg >= all) return false;
+  const int64_t t = wg < each * 8 ? (wg & 7) * each + (wg >> 3) : wg;
+  const int64_t group = t / (kGroup * col_tiles);
+  const int in = static_cast<int>(t - group * (kGroup * col_tiles));
+  const int64_t left = row_tiles - group * kGroup;
+  const int height = left < kGroup ? static_cast<int>(left) : kGroup;
+  col = in / height;
+  return find_tile(p, bm, group * kGroup + (in - col * height), out);
 }
 
 __device__ __forceinline__ int64_t source_row(const ProductArgs& p, int64_t row) {
@@ -260,30 +296,46 @@ __global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p,
 
 // ---- many rows: tiles through LDS --------------------------------------------------
 
-// BM tokens x BN weight rows (gated: BN / 2 outputs), WM x WN waves, K steps of
-// 64 through two stages of LDS filled by direct loads: one barrier per step,
-// behind which the next step's loads are requested.  A token row of a stage is
-// 128 bytes whose eight 16-byte chunks are stored at chunk ^ (row / 2) % 8, so the
-// 16 rows that a read touches lie in 16 different bank groups; rows past the
-// tile's end repeat its last one, inputs past K read zeros.
+// BM tokens x BN weight rows (gated: BN / 2 outputs), K steps of 32 through a ring
+// of S stages of LDS filled by direct loads.  A token row of a stage is 64 bytes
+// whose four 16-byte chunks are stored at chunk ^ -(row / 4) % 4, so the lanes that
+// a read serves at a time lie in different bank groups; rows past the tile's end
+// repeat its last one, inputs past K read zeros.
+//
+// The waves form two groups, one wave of each on every SIMD, half a step apart:
+// while one group's matrix instructions run, the other reads its next operands
+// from LDS and requests a later step's loads; a barrier swaps them.  In halves of
+// steps counted from the start, group 0 reads step h in half 2 h and multiplies in
+// 2 h + 1, group 1 one half later.  So stage h % S is read by all after half 2 h + 1
+// and takes the loads of step h + S from half 2 h + 2 on (in the group's read of
+// step h + 1), and what a wave requested for step h + 1 has to be there before half
+// 2 h + 2: it waits for that at the end of its read of step h.
 __device__ __align__(16) const uint16_t g_zeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 
-template <int BM, int BN, int WM, int WN, bool GATED>
-__global__ __launch_bounds__(64 * WM * WN) void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
+template <int N>
+__device__ __forceinline__ void wait_all_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int BM, int BN, int WM, int WN, int S, bool GATED>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2)))
+void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
   constexpr int NT = 64 * WM * WN;
   constexpr int NB = GATED ? 4 : 2;                 // blocks per strip
   constexpr int WTM = BM / WM, WTN = BN / WN;
   constexpr int TB = WTM / 16, RB = WTN / 16;
-  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
-  constexpr int JA = BM * 8 / NT, JB = BN * 8 / NT;
+  constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, STAGE = A_BYTES + B_BYTES;
+  constexpr int JA = BM * 4 / NT, JB = BN * 4 / NT, J = JA + JB;
   constexpr int TS = BN / 16 / NB;                  // strips per tile
-  static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0 && RB % NB == 0 && WTM % 16 == 0, "tile shape");
-  __shared__ __align__(16) char smem[2 * STAGE];
+  static_assert(WM * WN == 8, "two groups of four waves");
+  static_assert(BM * 4 % NT == 0 && BN * 4 % NT == 0 && JA > 0 && JB > 0 && RB % NB == 0 && WTM % 16 == 0, "tile shape");
+  static_assert(S >= 3 && J * (S - 2) < 64, "stages");
+  __shared__ __align__(16) char smem[S * STAGE];
 
   Tile tile;
-  const int64_t t = blockIdx.x / col_tiles;
-  const int strip0 = static_cast<int>(blockIdx.x - t * col_tiles) * TS;
-  if (!find_tile(p, BM, t, tile)) return;
+  int col;
+  if (!tile_of(p, BM, col_tiles, tile, col)) return;
+  const int strip0 = col * TS;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -293,64 +345,89 @@ __global__ __launch_bounds__(64 * WM * WN) void token_tile_kernel(ProductArgs p,
   int a_k[JA];
 #pragma unroll
   for (int j = 0; j < JA; ++j) {
-    const int r = (j * NT + tid) >> 3;
-    const int chunk = (tid & 7) ^ ((r >> 1) & 7);
+    const int r = (j * NT + tid) >> 2;
+    const int chunk = ((tid & 3) ^ -(r >> 2)) & 3;
     a_k[j] = chunk * 8;
     a_src[j] = p.x + source_row(p, tile.row0 + (r < tile.rows ? r : tile.rows - 1)) * p.ldx + chunk * 8;
   }
-  // the weights' blocks: a strip's two steps of 32 are contiguous
-  const uint16_t* b_src[JB];
+  const uint16_t* const b_base = p.w + (static_cast<int64_t>(tile.expert) * strips + strip0) * steps * (NB * kFrag);
+  uint32_t b_off[JB];
 #pragma unroll
   for (int j = 0; j < JB; ++j) {
     const int q = (j * NT + tid) >> 6;              // block of the stage
-    int s = strip0 + q / (2 * NB);
-    s = s < strips ? s : strips - 1;
-    b_src[j] = p.w + ((static_cast<int64_t>(tile.expert) * strips + s) * steps * NB + q % (2 * NB)) * kFrag + lane * 8;
+    int s = q / NB;
+    s = strip0 + s < strips ? s : strips - 1 - strip0;
+    b_off[j] = (static_cast<uint32_t>(s) * steps * NB + q % NB) * (kFrag * 2) + lane * 16;
   }
-  auto load = [&](int kt, char* stage) __attribute__((always_inline)) {
+  auto load = [&](int h, char* stage) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < JA; ++j) {
-      const uint16_t* src = a_src[j] + kt * 64;
-      if (kt * 64 + a_k[j] >= p.K) src = g_zeros;
+      const uint16_t* src = a_src[j] + h * 32;
+      if (h * 32 + a_k[j] >= p.K) src = g_zeros;
       load_lds16(src, stage + (j * NT + wave * 64) * 16);
     }
 #pragma unroll
     for (int j = 0; j < JB; ++j)
-      load_lds16(b_src[j] + static_cast<int64_t>(kt) * (2 * NB * kFrag), stage + A_BYTES + (j * NT + wave * 64) * 16);
+      load_lds16(b_base, b_off[j] + static_cast<uint32_t>(h) * (NB * kFrag * 2), stage + A_BYTES + (j * NT + wave * 64) * 16);
   };
+  const int xr = wm * WTM + (lane & 15);
+  const int x_at = xr * 64 + (((lane >> 4) ^ -(xr >> 2)) & 3) * 16, w_at = A_BYTES + wn * (RB * 1024) + lane * 16;
 
   f32x4 acc[TB][RB];
 #pragma unroll
   for (int b = 0; b < TB; ++b)
 #pragma unroll
     for (int c = 0; c < RB; ++c) acc[b][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bf16x8 x[TB], w[RB];
 
-  const int nk = steps / 2;
-  load(0, smem);
-  for (int kt = 0; kt < nk; ++kt) {
-    char* stage = smem + (kt & 1) * STAGE;
+  auto read = [&](const char* stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < RB; ++c) w[c] = *reinterpret_cast<const bf16x8*>(stage + w_at + c * 1024);
+#pragma unroll
+    for (int b = 0; b < TB; ++b) x[b] = *reinterpret_cast<const bf16x8*>(stage + x_at + b * 1024);
+  };
+  auto multiply = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int b = 0; b < TB; ++b)
+#pragma unroll
+      for (int c = 0; c < RB; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[c], x[b], acc[b][c], 0, 0, 0);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  const int nh = steps;
+#pragma unroll
+  for (int h = 0; h < S - 1; ++h)
+    if (h < nh) load(h, smem + h * STAGE);
+  if (nh >= S - 1)
+    wait_vm_barrier<J * (S - 2)>();
+  else
     wait_vm_barrier<0>();
-    if (kt + 1 < nk) load(kt + 1, smem + ((kt + 1) & 1) * STAGE);
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      bf16x8 xf[TB], wf[RB];
-#pragma unroll
-      for (int b = 0; b < TB; ++b) {
-        const int r = wm * WTM + b * 16 + (lane & 15);
-        const int chunk = (s * 4 + (lane >> 4)) ^ ((r >> 1) & 7);
-        xf[b] = *reinterpret_cast<const bf16x8*>(stage + r * 128 + chunk * 16);
-      }
-#pragma unroll
-      for (int c = 0; c < RB; ++c) {
-        const int blk = wn * RB + c;                // block of the tile: strip blk / NB
-        wf[c] = *reinterpret_cast<const bf16x8*>(stage + A_BYTES + ((blk / NB * 2 + s) * NB + blk % NB) * 1024 + lane * 16);
-      }
-#pragma unroll
-      for (int b = 0; b < TB; ++b)
-#pragma unroll
-        for (int c = 0; c < RB; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c], xf[b], acc[b][c], 0, 0, 0);
-    }
+  if (wave >= 4) lds_barrier();                     // group 1 is half a step behind
+
+  // step h reads stage h % S (`cur`) and loads step h + S - 1 into the stage before it
+  char* cur = smem;
+  char* prev = smem + (S - 1) * STAGE;
+  int h = 0;
+  for (; h + S - 1 < nh; ++h) {
+    read(cur);
+    load(h + S - 1, prev);
+    wait_all_barrier<J * (S - 2)>();
+    multiply();
+    lds_barrier();
+    prev = cur;
+    cur = cur == smem + (S - 1) * STAGE ? smem : cur + STAGE;
   }
+  for (; h < nh; ++h) {
+    read(cur);
+    wait_all_barrier<0>();
+    multiply();
+    lds_barrier();
+    cur = cur == smem + (S - 1) * STAGE ? smem : cur + STAGE;
+  }
+  if (wave < 4) lds_barrier();
 
 #pragma unroll
   for (int b = 0; b < TB; ++b) {
@@ -423,11 +500,12 @@ void skinny(const ProductArgs& a, hipStream_t s) {
   token_skinny_kernel<TB, GATED, 4><<<static_cast<unsigned>(row_tiles(a, 16 * TB) * strips), 256, 0, s>>>(a, strips, steps);
 }
 
-template <int BM, int BN, int WM, int WN, bool GATED>
+template <int BM, int BN, int WM, int WN, int S, bool GATED>
 void tiles(const ProductArgs& a, hipStream_t s) {
   const int strips = strips_of(a.N), steps = steps_of(a.K), per = BN / (GATED ? 64 : 32);
   const int cols = (strips + per - 1) / per;
-  token_tile_kernel<BM, BN, WM, WN, GATED><<<static_cast<unsigned>(row_tiles(a, BM) * cols), 64 * WM * WN, 0, s>>>(a, strips, steps, cols);
+  token_tile_kernel<BM, BN, WM, WN, S, GATED>
+      <<<static_cast<unsigned>(row_tiles(a, BM) * cols), 64 * WM * WN, 0, s>>>(a, strips, steps, cols);
 }
 
 template <bool GATED>
@@ -435,8 +513,11 @@ void product(const ProductArgs& a, hipStream_t s) {
   const int64_t per = a.offsets ? a.rows / a.experts : a.rows;     // rows of a layer, on average
   if (per <= 16) return skinny<1, GATED>(a, s);
   if (per <= 32) return skinny<2, GATED>(a, s);
-  if (per <= 512) return tiles<128, 128, 2, 2, GATED>(a, s);
-  tiles<256, 256, 2, 4, GATED>(a, s);
+#ifndef SX
+#define SX 4
+#endif
+  if (per <= 512) return tiles<128, 256, 2, 4, SX, GATED>(a, s);
+  tiles<256, 256, 2, 4, SX, GATED>(a, s);
 }
 
 }  // namespace
