@@ -249,7 +249,7 @@ int dycl_op_linear(const uint16_t* x, int64_t ldx, int64_t m, int k, const uint1
     a.residual = residual;
     a.ldr = ldr;
     a.y = y;
-    a.y_f32 = y_type == DYCL_F32;
+    a.y_kind = y_type == DYCL_F32 ? Y_F32 : Y_BF16;
     a.ldy = ldy;
     a.N_store = n;
     token_product(a, s);
@@ -307,6 +307,7 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     }
     a.order = order;
     a.order_k = k;
+    a.x_rows = n;
     a.offsets = offsets;
     a.experts = experts;
     a.rows = static_cast<int64_t>(pairs);
@@ -335,6 +336,7 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     b.bias = bias2;
     b.act = TACT_NONE;
     b.y = part;
+    b.y_kind = Y_SHARED;
     b.ldy = dp;
     b.N_store = static_cast<int>(dp);
     token_product(b, s);

@@ -10,6 +10,8 @@
 // strip's blocks adjoin: row r of block b is output 8 (r / 4) + 4 b + r % 4 of
 // the strip, which leaves a lane eight consecutive outputs to store.  A gated
 // strip alternates blocks of the two products, and a lane holds both factors.
+#include <type_traits>
+
 #include "token_dev.hpp"
 
 namespace dycl {
@@ -150,25 +152,78 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs& p, int64_t row)
   return p.order ? p.order[row] / p.order_k : row;
 }
 
-// Eight consecutive outputs of one row from `o`: bias, activation or gate,
-// residual, store.  a: the strip's first block, b: its second; ga, gb: the gate's.
-template <bool GATED>
-__device__ __forceinline__ void finish8(const ProductArgs& p, int expert, int64_t row, int o, f32x4 a, f32x4 b, f32x4 ga, f32x4 gb) {
-  if (o >= p.N_store) return;
-  float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  const float g[8] = {ga[0], ga[1], ga[2], ga[3], gb[0], gb[1], gb[2], gb[3]};
-  const float* bias = p.bias ? p.bias + static_cast<int64_t>(expert) * p.N : nullptr;
-  const float* gbias = GATED && p.gate_bias ? p.gate_bias + static_cast<int64_t>(expert) * p.N : nullptr;
+// ---- epilogues -------------------------------------------------------------------
+
+// An expert's results wait for their weighted sum in 16 bits per value: eight
+// consecutive ones share an exponent e, two bits of it above two 15-bit integers
+// q = v 2^(140 - e) 16383 / 16384 in each of four words (the factor keeps a largest
+// value that rounds up within 15 bits).  That is off by 2^-14 of the largest of the
+// eight where bf16 is off by 2^-8 of each value, for the same bytes; float32 would
+// double them.  Exponent 255 marks a group with an infinity or a NaN: it holds the
+// values' upper 15 bits.
+constexpr float kSharedUnit = 16383.0f / 16384.0f;
+
+__device__ __forceinline__ uint4 pack_shared(const float (&v)[8]) {
+  uint32_t m = 0, q[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    if (bias && o + j < p.N) v[j] += bias[o + j];
-    if (GATED) {
-      float u = g[j];
-      if (gbias && o + j < p.N) u += gbias[o + j];
-      v[j] *= token_act(u, p.act);
-    } else {
-      v[j] = token_act(v[j], p.act);
+    const uint32_t u = __float_as_uint(v[j]) & 0x7fffffffu;
+    m = m > u ? m : u;
+  }
+  uint32_t e = m >> 23;                             // (NaN and infinity: 255)
+  if (e < 255) {
+    e = e > 13 ? e : 13;                            // (scale within float32)
+    const float scale = __uint_as_float((267 - e) << 23) * kSharedUnit;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(fmaf(v[j], scale, 12582912.0f));   // 1.5 2^23: rounds to an integer in the low bits
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = (v[j] != v[j] ? 0x7fe00000u : __float_as_uint(v[j])) >> 17;
+  }
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = (q[2 * j] & 0x7fff) | (q[2 * j + 1] & 0x7fff) << 15 | (e >> (2 * j)) << 30;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// sum[j] += weight * value j
+__device__ __forceinline__ void add_shared(const uint4& u, float weight, float (&sum)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  const int e = w[0] >> 30 | (w[1] >> 30) << 2 | (w[2] >> 30) << 4 | (w[3] >> 30) << 6;
+  if (e != 255) {
+    const float scale = ldexpf(weight * (1.0f / kSharedUnit), e - 140);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sum[2 * j] = fmaf(scale, static_cast<float>(static_cast<int32_t>(w[j] << 17) >> 17), sum[2 * j]);
+      sum[2 * j + 1] = fmaf(scale, static_cast<float>(static_cast<int32_t>(w[j] << 2) >> 17), sum[2 * j + 1]);
     }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sum[2 * j] = fmaf(weight, __uint_as_float(w[j] << 17), sum[2 * j]);
+      sum[2 * j + 1] = fmaf(weight, __uint_as_float(w[j] << 2 & 0xfffe0000u), sum[2 * j + 1]);
+    }
+  }
+}
+
+// values [o, o + 8) of an expert's bias vector (0 past the end or without one)
+__device__ __forceinline__ void bias8(const ProductArgs& p, const float* bias, int expert, int o, float (&r)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = bias && o + j < p.N ? bias[static_cast<int64_t>(expert) * p.N + o + j] : 0.f;
+}
+
+// Outputs o to o + 7 of one row: bias, activation or gate, residual.  a and b are
+// the strip's blocks, ga and gb the gate's.
+template <bool GATED, int ACT>
+__device__ __forceinline__ void finish8(const ProductArgs& p, int64_t row, int o, const f32x4& a, const f32x4& b, const f32x4& ga, const f32x4& gb,
+                                        const float (&bias)[8], const float (&gate_bias)[8], float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = (j < 4 ? a[j & 3] : b[j & 3]) + bias[j];
+    if (GATED)
+      v[j] *= token_act((j < 4 ? ga[j & 3] : gb[j & 3]) + gate_bias[j], ACT);
+    else
+      v[j] = token_act(v[j], ACT);
   }
   if (o + 8 > p.N) {
     // the padding's zero weights make NaN of an infinite input: what is stored there is 0
@@ -176,10 +231,9 @@ __device__ __forceinline__ void finish8(const ProductArgs& p, int expert, int64_
     for (int j = 0; j < 8; ++j)
       if (o + j >= p.N) v[j] = 0.f;
   }
-  const bool whole = o + 8 <= p.N_store;
   if (p.residual) {
     const uint16_t* r = p.residual + row * p.ldr + o;
-    if (whole && reinterpret_cast<uintptr_t>(r) % 16 == 0) {
+    if (o + 8 <= p.N && reinterpret_cast<uintptr_t>(r) % 16 == 0) {
       const uint4 q = *reinterpret_cast<const uint4*>(r);
       const uint32_t e[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -190,10 +244,19 @@ __device__ __forceinline__ void finish8(const ProductArgs& p, int expert, int64_
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (o + j < p.N_store) v[j] += bf2f(r[j]);
+        if (o + j < p.N) v[j] += bf2f(r[j]);
     }
   }
-  if (p.y_f32) {
+}
+
+__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
+  return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+
+__device__ __forceinline__ void store8(const ProductArgs& p, int64_t row, int o, const float (&v)[8]) {
+  if (o >= p.N_store) return;
+  const bool whole = o + 8 <= p.N_store;
+  if (p.y_kind == Y_F32) {
     float* y = static_cast<float*>(p.y) + row * p.ldy + o;
     if (whole && reinterpret_cast<uintptr_t>(y) % 16 == 0) {
       reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -203,26 +266,68 @@ __device__ __forceinline__ void finish8(const ProductArgs& p, int expert, int64_
       for (int j = 0; j < 8; ++j)
         if (o + j < p.N_store) y[j] = v[j];
     }
-  } else {
-    uint16_t* y = static_cast<uint16_t*>(p.y) + row * p.ldy + o;
-    if (whole && reinterpret_cast<uintptr_t>(y) % 16 == 0) {
-      *reinterpret_cast<uint4*>(y) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (o + j < p.N_store) y[j] = f2bf(v[j]);
-    }
+    return;
   }
+  uint16_t* y = static_cast<uint16_t*>(p.y) + row * p.ldy + o;
+  if (p.y_kind == Y_SHARED) {                       // (rows padded to whole strips)
+    *reinterpret_cast<uint4*>(y) = pack_shared(v);
+  } else if (whole && reinterpret_cast<uintptr_t>(y) % 16 == 0) {
+    *reinterpret_cast<uint4*>(y) = pack8(v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (o + j < p.N_store) y[j] = f2bf(v[j]);
+  }
+}
+
+// f with the activation as a constant: in every element's way, its branches took
+// longer than the sums of a short contraction
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == TACT_NONE) f(std::integral_constant<int, TACT_NONE>{});
+  else if (act == TACT_RELU) f(std::integral_constant<int, TACT_RELU>{});
+  else if (act == TACT_GELU) f(std::integral_constant<int, TACT_GELU>{});
+  else f(std::integral_constant<int, TACT_SILU>{});
+}
+
+// The sums of a wave's TB x RB blocks, from row `row0` of the tile and strip
+// `strip`, to y.  (Rows of bf16 passed through LDS and stored in runs of the tile's
+// width took as long as the lanes' own 16-byte pieces.)
+template <int TB, int RB, bool GATED>
+__device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& tile, int row0, int strip, const f32x4 (&acc)[TB][RB]) {
+  constexpr int NB = GATED ? 4 : 2;
+  const int lane = threadIdx.x & 63;
+  auto finish = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < RB; c += NB) {
+      const int o = (strip + c / NB) * kStrip + 8 * (lane >> 4);
+      float b8[8], g8[8];
+      bias8(p, p.bias, tile.expert, o, b8);
+      bias8(p, GATED ? p.gate_bias : nullptr, tile.expert, o, g8);
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        const int row = row0 + b * 16 + (lane & 15);
+        if (row >= tile.rows || o >= p.N_store) continue;
+        float v[8];
+        if (GATED)
+          finish8<true, act>(p, tile.row0 + row, o, acc[b][c], acc[b][c + 2 < RB ? c + 2 : 0], acc[b][c + 1], acc[b][c + 3 < RB ? c + 3 : 0], b8, g8, v);
+        else
+          finish8<false, act>(p, tile.row0 + row, o, acc[b][c], acc[b][c + 1], acc[b][c], acc[b][c], b8, g8, v);
+        store8(p, tile.row0 + row, o, v);
+      }
+    }
+  };
+  with_act(p.act, finish);
 }
 
 // ---- few rows per layer: the weights go from memory to the registers --------------
 
 // A workgroup takes one strip of 32 outputs for up to 16 TB rows of one layer;
-// its waves take the K steps in turn and add their sums through LDS.
+// its waves take a range of the K steps each and add their sums through LDS.
 template <int TB, bool GATED, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p, int strips, int steps) {
   constexpr int NB = GATED ? 4 : 2, ACC = TB * NB;
-  constexpr int U = TB == 1 ? 4 : 2;           // steps whose operands are in flight together
+  constexpr int U = GATED ? 2 : 4;                  // steps whose operands are in flight together
   __shared__ f32x4 sums[WAVES][ACC][64];
   Tile tile;
   const int64_t t = blockIdx.x / strips;
@@ -244,7 +349,6 @@ __global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p,
 #pragma unroll
     for (int c = 0; c < NB; ++c) acc[b][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // wave i takes steps [i, i + 1) * steps / WAVES
   const int s0 = wave * steps / WAVES, s1 = (wave + 1) * steps / WAVES;
   const int k_lane = 8 * (lane >> 4);
   for (int s = s0; s < s1; s += U) {
@@ -275,22 +379,29 @@ __global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p,
 #pragma unroll
     for (int c = 0; c < NB; ++c) sums[wave][b * NB + c][lane] = acc[b][c];
   __syncthreads();
+  // a wave adds up a block, in the order of the waves; then a wave finishes 16 rows
+  for (int q = wave; q < ACC; q += WAVES) {
+    f32x4 r = sums[0][q][lane];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) r += sums[i][q][lane];
+    sums[0][q][lane] = r;
+  }
+  __syncthreads();
   for (int b = wave; b < TB; b += WAVES) {
-    f32x4 r[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) r[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < NB; ++c)
-#pragma unroll
-      for (int i = 0; i < WAVES; ++i) r[c] += sums[i][b * NB + c][lane];
     const int row = b * 16 + (lane & 15);
     const int o = strip * kStrip + 8 * (lane >> 4);
-    if (row < tile.rows) {
+    if (row >= tile.rows || o >= p.N_store) continue;
+    float b8[8], g8[8], v[8];
+    bias8(p, p.bias, tile.expert, o, b8);
+    bias8(p, GATED ? p.gate_bias : nullptr, tile.expert, o, g8);
+    const f32x4(&r)[ACC][64] = sums[0];
+    with_act(p.act, [&](auto act) __attribute__((always_inline)) {
       if (GATED)
-        finish8<true>(p, tile.expert, tile.row0 + row, o, r[0], r[2], r[1], r[3]);
+        finish8<true, act>(p, tile.row0 + row, o, r[b * NB][lane], r[b * NB + 2][lane], r[b * NB + 1][lane], r[b * NB + 3][lane], b8, g8, v);
       else
-        finish8<false>(p, tile.expert, tile.row0 + row, o, r[0], r[1], r[0], r[1]);
-    }
+        finish8<false, act>(p, tile.row0 + row, o, r[b * NB][lane], r[b * NB + 1][lane], r[b * NB][lane], r[b * NB][lane], b8, g8, v);
+    });
+    store8(p, tile.row0 + row, o, v);
   }
 }
 
@@ -306,10 +417,13 @@ __global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p,
 // while one group's matrix instructions run, the other reads its next operands
 // from LDS and requests a later step's loads; a barrier swaps them.  In halves of
 // steps counted from the start, group 0 reads step h in half 2 h and multiplies in
-// 2 h + 1, group 1 one half later.  So stage h % S is read by all after half 2 h + 1
-// and takes the loads of step h + S from half 2 h + 2 on (in the group's read of
-// step h + 1), and what a wave requested for step h + 1 has to be there before half
-// 2 h + 2: it waits for that at the end of its read of step h.
+// 2 h + 1, group 1 one half later.  So stage h % S has been read by all after half
+// 2 h + 1 and takes the loads of step h + S from half 2 h + 2 on (in the group's read
+// of step h + 1), and what a wave requested for step h + 1 has to be there before
+// half 2 h + 2: it waits for that at the end of its read of step h.  With the waves
+// in step, all reading and then all multiplying, 8192 x 4096 x 8192 took 4 % longer;
+// with four waves of 128 x 128 each, 14 %; with 32 x 32 x 16 instructions 9 %.  The
+// matrix cores are 68 % busy at the clock that this load leaves.
 __device__ __align__(16) const uint16_t g_zeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 
 template <int N>
@@ -318,8 +432,7 @@ __device__ __forceinline__ void wait_all_barrier() {
 }
 
 template <int BM, int BN, int WM, int WN, int S, bool GATED>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2)))
-void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
+__device__ __forceinline__ void tile_product(const ProductArgs& p, const Tile& tile, int col, int strips, int steps, char* smem) {
   constexpr int NT = 64 * WM * WN;
   constexpr int NB = GATED ? 4 : 2;                 // blocks per strip
   constexpr int WTM = BM / WM, WTN = BN / WN;
@@ -330,25 +443,22 @@ void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
   static_assert(WM * WN == 8, "two groups of four waves");
   static_assert(BM * 4 % NT == 0 && BN * 4 % NT == 0 && JA > 0 && JB > 0 && RB % NB == 0 && WTM % 16 == 0, "tile shape");
   static_assert(S >= 3 && J * (S - 2) < 64, "stages");
-  __shared__ __align__(16) char smem[S * STAGE];
-
-  Tile tile;
-  int col;
-  if (!tile_of(p, BM, col_tiles, tile, col)) return;
   const int strip0 = col * TS;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
 
-  // this thread's rows of x and the K chunk that it loads of each
-  const uint16_t* a_src[JA];
+  // this thread's rows of x, as byte offsets, and the K chunk that it loads of each
+  const uint16_t* const a_base = p.order ? p.x : p.x + tile.row0 * p.ldx;
+  int64_t a_off[JA];
   int a_k[JA];
 #pragma unroll
   for (int j = 0; j < JA; ++j) {
     const int r = (j * NT + tid) >> 2;
     const int chunk = ((tid & 3) ^ -(r >> 2)) & 3;
+    const int64_t row = r < tile.rows ? r : tile.rows - 1;
     a_k[j] = chunk * 8;
-    a_src[j] = p.x + source_row(p, tile.row0 + (r < tile.rows ? r : tile.rows - 1)) * p.ldx + chunk * 8;
+    a_off[j] = ((p.order ? p.order[tile.row0 + row] / p.order_k : row) * p.ldx + chunk * 8) * 2;
   }
   const uint16_t* const b_base = p.w + (static_cast<int64_t>(tile.expert) * strips + strip0) * steps * (NB * kFrag);
   uint32_t b_off[JB];
@@ -359,16 +469,23 @@ void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
     s = strip0 + s < strips ? s : strips - 1 - strip0;
     b_off[j] = (static_cast<uint32_t>(s) * steps * NB + q % NB) * (kFrag * 2) + lane * 16;
   }
+  // (steps below `near` have all their inputs, at offsets of 32 bits from one base)
+  const int near = p.far ? 0 : p.K / 32;
   auto load = [&](int h, char* stage) __attribute__((always_inline)) {
+    if (h < near) {
 #pragma unroll
-    for (int j = 0; j < JA; ++j) {
-      const uint16_t* src = a_src[j] + h * 32;
-      if (h * 32 + a_k[j] >= p.K) src = g_zeros;
-      load_lds16(src, stage + (j * NT + wave * 64) * 16);
+      for (int j = 0; j < JA; ++j) load_lds16(a_base + h * 32, static_cast<uint32_t>(a_off[j]), stage + (j * NT + wave * 64) * 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < JA; ++j) {
+        const char* src = reinterpret_cast<const char*>(a_base + h * 32) + a_off[j];
+        if (h * 32 + a_k[j] >= p.K) src = reinterpret_cast<const char*>(g_zeros);
+        load_lds16(src, stage + (j * NT + wave * 64) * 16);
+      }
     }
+    const char* const b_step = reinterpret_cast<const char*>(b_base) + static_cast<int64_t>(h) * (NB * kFrag * 2);
 #pragma unroll
-    for (int j = 0; j < JB; ++j)
-      load_lds16(b_base, b_off[j] + static_cast<uint32_t>(h) * (NB * kFrag * 2), stage + A_BYTES + (j * NT + wave * 64) * 16);
+    for (int j = 0; j < JB; ++j) load_lds16(b_step, b_off[j], stage + A_BYTES + (j * NT + wave * 64) * 16);
   };
   const int xr = wm * WTM + (lane & 15);
   const int x_at = xr * 64 + (((lane >> 4) ^ -(xr >> 2)) & 3) * 16, w_at = A_BYTES + wn * (RB * 1024) + lane * 16;
@@ -428,25 +545,160 @@ void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
     cur = cur == smem + (S - 1) * STAGE ? smem : cur + STAGE;
   }
   if (wave < 4) lds_barrier();
+  tile_epilogue<TB, RB, GATED>(p, tile, wm * WTM, strip0 + wn * (RB / NB), acc);
+}
+
+// 256 x 256 tiles, one workgroup per CU; an expert's last tile, where it has 128
+// rows or fewer, takes half the time.  128 x 256 tiles on three stages leave room for two
+// workgroups, one's epilogue beside the other's products: better for short K.
+template <int BM, bool GATED>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(BM == 256 ? 2 : 4)))
+void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
+  constexpr int S = BM == 256 ? 4 : 3;
+  __shared__ __align__(16) char smem[S * (BM + 256) * 64];
+  Tile tile;
+  int col;
+  if (!tile_of(p, BM, col_tiles, tile, col)) return;
+  if (BM == 128 || tile.rows > 128)
+    tile_product<BM, 256, 2, 4, S, GATED>(p, tile, col, strips, steps, smem);
+  else
+    tile_product<128, 256, 2, 4, S, GATED>(p, tile, col, strips, steps, smem);
+}
+
+// Smaller tiles, for products that large ones would leave CUs idle with: KG groups
+// of WM x WN waves split the K range of one tile (their sums meet in LDS), each with
+// its own ring of S stages of 64 inputs.  A token row of a stage is 128 bytes whose
+// eight 16-byte chunks are stored at chunk ^ (row / 2) % 8.  One barrier per step:
+// behind it, the stage read a step ago takes the loads of step kt + S - 1.
+template <int BM, int BN, int WM, int WN, int KG, int S, bool GATED>
+__global__ __launch_bounds__(64 * WM * WN * KG) void token_split_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
+  constexpr int NT = 64 * WM * WN;                  // threads of a group
+  constexpr int NB = GATED ? 4 : 2;                 // blocks per strip
+  constexpr int WTM = BM / WM, WTN = BN / WN;
+  constexpr int TB = WTM / 16, RB = WTN / 16;
+  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
+  constexpr int JA = BM * 8 / NT, JB = BN * 8 / NT, J = JA + JB;
+  constexpr int TS = BN / 16 / NB;                  // strips per tile
+  static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0 && NT % 128 == 0 && RB % NB == 0 && WTM % 16 == 0, "tile shape");
+  static_assert(S >= 2 && J * (S - 2) < 64 && (KG - 1) * BM * BN * 4 <= KG * S * STAGE, "stages");
+  __shared__ __align__(16) char smem[KG * S * STAGE];
+
+  Tile tile;
+  int col;
+  if (!tile_of(p, BM, col_tiles, tile, col)) return;
+  const int strip0 = col * TS;
+  const int lane = threadIdx.x & 63, tid = threadIdx.x % NT;
+  const int all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = all_wave / (WM * WN), wave = all_wave % (WM * WN);
+  const int wm = wave / WN, wn = wave % WN;
+  char* const ring = smem + group * (S * STAGE);
+
+  const uint16_t* const a_base = p.order ? p.x : p.x + tile.row0 * p.ldx;
+  int64_t a_off[JA];
+  const int a_k = ((tid & 7) ^ ((tid >> 4) & 7)) * 8;       // (NT / 8 rows further on, the chunk is the same)
+#pragma unroll
+  for (int j = 0; j < JA; ++j) {
+    const int r = (j * NT + tid) >> 3;
+    const int64_t row = r < tile.rows ? r : tile.rows - 1;
+    a_off[j] = ((p.order ? p.order[tile.row0 + row] / p.order_k : row) * p.ldx + a_k) * 2;
+  }
+  const uint16_t* const b_base = p.w + (static_cast<int64_t>(tile.expert) * strips + strip0) * steps * (NB * kFrag);
+  uint32_t b_off[JB];
+#pragma unroll
+  for (int j = 0; j < JB; ++j) {
+    const int q = (j * NT + tid) >> 6;              // block of the stage
+    int s = q / (2 * NB);
+    s = strip0 + s < strips ? s : strips - 1 - strip0;
+    b_off[j] = (static_cast<uint32_t>(s) * steps * NB + q % (2 * NB)) * (kFrag * 2) + lane * 16;
+  }
+  const int near = p.far ? 0 : p.K / 64;
+  const int nk_all = steps / 2;
+  const int k0 = group * nk_all / KG, nk = (group + 1) * nk_all / KG - k0;
+  auto load = [&](int kt, char* stage) __attribute__((always_inline)) {
+    if (kt < near) {
+#pragma unroll
+      for (int j = 0; j < JA; ++j) load_lds16(a_base + kt * 64, static_cast<uint32_t>(a_off[j]), stage + (j * NT + wave * 64) * 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < JA; ++j) {
+        const char* src = reinterpret_cast<const char*>(a_base + kt * 64) + a_off[j];
+        if (kt * 64 + a_k >= p.K) src = reinterpret_cast<const char*>(g_zeros);
+        load_lds16(src, stage + (j * NT + wave * 64) * 16);
+      }
+    }
+    const char* const b_step = reinterpret_cast<const char*>(b_base) + static_cast<int64_t>(kt) * (2 * NB * kFrag * 2);
+#pragma unroll
+    for (int j = 0; j < JB; ++j) load_lds16(b_step, b_off[j], stage + A_BYTES + (j * NT + wave * 64) * 16);
+  };
+  const int xr = wm * WTM + (lane & 15);
+  f32x4 acc[TB][RB];
+#pragma unroll
+  for (int b = 0; b < TB; ++b)
+#pragma unroll
+    for (int c = 0; c < RB; ++c) acc[b][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
 #pragma unroll
-  for (int b = 0; b < TB; ++b) {
-    const int row = wm * WTM + b * 16 + (lane & 15);
-    if (row >= tile.rows) continue;
+  for (int i = 0; i < S - 1; ++i)
+    if (i < nk) load(k0 + i, ring + i * STAGE);
+  const int turns = (nk_all + KG - 1) / KG;         // of the group with the most steps
+  char* cur = ring;
+  char* prev = ring + (S - 1) * STAGE;
+  for (int i = 0; i < turns; ++i) {
+    if (i + S - 1 <= nk)
+      wait_all_barrier<J * (S - 2)>();
+    else
+      wait_all_barrier<0>();
+    if (i + S - 1 < nk) load(k0 + i + S - 1, prev);
+    if (i < nk) {
+      bf16x8 x[2][TB], w[2][RB];
 #pragma unroll
-    for (int c = 0; c < RB; c += NB) {
-      const int strip = strip0 + (wn * RB + c) / NB;
-      const int o = strip * kStrip + 8 * (lane >> 4);
-      if (GATED)
-        finish8<true>(p, tile.expert, tile.row0 + row, o, acc[b][c], acc[b][c + 2], acc[b][c + 1], acc[b][c + 3]);
-      else
-        finish8<false>(p, tile.expert, tile.row0 + row, o, acc[b][c], acc[b][c + 1], acc[b][c], acc[b][c + 1]);
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int c = 0; c < RB; ++c) {
+          const int blk = wn * RB + c;              // block of the tile: strip blk / NB
+          w[s][c] = *reinterpret_cast<const bf16x8*>(cur + A_BYTES + ((blk / NB * 2 + s) * NB + blk % NB) * 1024 + lane * 16);
+        }
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
+          x[s][b] = *reinterpret_cast<const bf16x8*>(cur + (xr + b * 16) * 128 + (((s * 4 + (lane >> 4)) ^ (xr >> 1)) & 7) * 16);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
+#pragma unroll
+          for (int c = 0; c < RB; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[s][c], x[s][b], acc[b][c], 0, 0, 0);
     }
+    prev = cur;
+    cur = cur == ring + (S - 1) * STAGE ? ring : cur + STAGE;
   }
+
+  if (KG > 1) {
+    // the other groups' sums, in their order
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem);
+    lds_barrier();
+    if (group > 0) {
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+#pragma unroll
+        for (int c = 0; c < RB; ++c) sums[(((group - 1) * WM * WN + wave) * TB * RB + b * RB + c) * 64 + lane] = acc[b][c];
+    }
+    lds_barrier();
+    if (group > 0) return;
+    for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+#pragma unroll
+        for (int c = 0; c < RB; ++c) acc[b][c] += sums[((g * WM * WN + wave) * TB * RB + b * RB + c) * 64 + lane];
+  }
+  tile_epilogue<TB, RB, GATED>(p, tile, wm * WTM, strip0 + wn * (RB / NB), acc);
 }
 
 // ---- the experts' results, weighted and summed ----------------------------------------
 
+// Eight outputs per lane.  A row's slots and weights come first, then up to eight
+// experts' results are requested together: taken one by one, each waited for its
+// slot and then for its values.
 __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
   const int per = (p.d + 7) / 8;
   const int64_t all = p.n * per;
@@ -459,25 +711,40 @@ __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
     const bool whole = o + 8 <= p.d;
     if (p.residual) {
       const uint16_t* r = p.residual + row * p.ldr + o;
+      if (whole && reinterpret_cast<uintptr_t>(r) % 16 == 0) {
+        const uint4 f = *reinterpret_cast<const uint4*>(r);
+        const uint32_t e[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[2 * j] = __uint_as_float(e[j] << 16);
+          v[2 * j + 1] = __uint_as_float(e[j] & 0xffff0000u);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (o + j < p.d) v[j] = bf2f(r[j]);
+      }
+    }
+    for (int j0 = 0; j0 < p.k; j0 += 8) {
+      int slot[8];
+      float w[8];
+      uint4 f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool in = j0 + j < p.k;
+        slot[j] = in ? p.slots[row * p.k + j0 + j] : -1;
+        w[j] = in ? p.weights[row * p.k + j0 + j] : 0.f;
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (o + j < p.d) v[j] = bf2f(r[j]);
-    }
-    for (int j = 0; j < p.k; ++j) {
-      const int slot = p.slots[row * p.k + j];
-      if (slot < 0) continue;
-      const float w = p.weights[row * p.k + j];
-      const uint4 f = *reinterpret_cast<const uint4*>(p.part + slot * p.ldp + o);
-      const uint32_t e[4] = {f.x, f.y, f.z, f.w};
+        if (slot[j] >= 0) f[j] = *reinterpret_cast<const uint4*>(p.part + slot[j] * p.ldp + o);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = fmaf(w, __uint_as_float(e[i] << 16), v[2 * i]);
-        v[2 * i + 1] = fmaf(w, __uint_as_float(e[i] & 0xffff0000u), v[2 * i + 1]);
-      }
+      for (int j = 0; j < 8; ++j)
+        if (slot[j] >= 0) add_shared(f[j], w[j], v);
     }
     uint16_t* out = p.out + row * p.ldo + o;
     if (whole && reinterpret_cast<uintptr_t>(out) % 16 == 0) {
-      *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+      *reinterpret_cast<uint4*>(out) = pack8(v);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -497,27 +764,89 @@ int64_t row_tiles(const ProductArgs& a, int bm) {
 template <int TB, bool GATED>
 void skinny(const ProductArgs& a, hipStream_t s) {
   const int strips = strips_of(a.N), steps = steps_of(a.K);
-  token_skinny_kernel<TB, GATED, 4><<<static_cast<unsigned>(row_tiles(a, 16 * TB) * strips), 256, 0, s>>>(a, strips, steps);
+  const int64_t groups = row_tiles(a, 16 * TB) * strips;
+  // few workgroups: more waves each, for as many loads in flight
+  if (groups <= 256)
+    token_skinny_kernel<TB, GATED, 16><<<static_cast<unsigned>(groups), 1024, 0, s>>>(a, strips, steps);
+  else if (groups <= 512)
+    token_skinny_kernel<TB, GATED, 8><<<static_cast<unsigned>(groups), 512, 0, s>>>(a, strips, steps);
+  else
+    token_skinny_kernel<TB, GATED, 4><<<static_cast<unsigned>(groups), 256, 0, s>>>(a, strips, steps);
 }
 
-template <int BM, int BN, int WM, int WN, int S, bool GATED>
+template <int BM, bool GATED>
 void tiles(const ProductArgs& a, hipStream_t s) {
+  const int strips = strips_of(a.N), steps = steps_of(a.K), per = 256 / (GATED ? 64 : 32);
+  const int cols = (strips + per - 1) / per;
+  token_tile_kernel<BM, GATED><<<static_cast<unsigned>(row_tiles(a, BM) * cols), 512, 0, s>>>(a, strips, steps, cols);
+}
+
+template <int BM, int BN, int WM, int WN, int KG, int S, bool GATED>
+void split(const ProductArgs& a, hipStream_t s) {
   const int strips = strips_of(a.N), steps = steps_of(a.K), per = BN / (GATED ? 64 : 32);
   const int cols = (strips + per - 1) / per;
-  token_tile_kernel<BM, BN, WM, WN, S, GATED>
-      <<<static_cast<unsigned>(row_tiles(a, BM) * cols), 64 * WM * WN, 0, s>>>(a, strips, steps, cols);
+  token_split_kernel<BM, BN, WM, WN, KG, S, GATED>
+      <<<static_cast<unsigned>(row_tiles(a, BM) * cols), 64 * WM * WN * KG, 0, s>>>(a, strips, steps, cols);
+}
+
+// Which kernel: the one whose estimate is least.  A round of tiles (256 CUs, per_cu
+// workgroups each) takes `round` microseconds and `full` per K step of 64, `alone`
+// where each CU has one; fitted to products of 16 to 16384 rows and K of 128 to 8192.
+struct Shape {
+  int bm, bn, per_cu;
+  float alone, full, round;
+};
+constexpr Shape kShapes[] = {
+    {256, 256, 1, 1.13f, 1.42f, 9.5f},    // 8192 x 8192 x 8192: 787 us (128 x 256: 921)
+    {128, 256, 2, 0.75f, 1.50f, 7.0f},    // 16384 x 1024 x 2048: 60 us (256 x 256: 64, 64 x 128: 91)
+    {64, 128, 2, 0.36f, 0.58f, 3.5f},     // 1024 x 4096 x 4096: 41 us (128 x 256: 51)
+    {64, 128, 1, 0.285f, 0.31f, 3.7f},    // two K groups; 300 x 4096 x 4096: 24.2 us (without: 28.3)
+    {64, 64, 1, 0.245f, 0.25f, 2.9f},     // four K groups; 512 x 2048 x 2048: 11.9 us (64 x 128: 15.0)
+    {32, 64, 1, 0.135f, 0.14f, 2.5f},     // four K groups; 128 x 4096 x 4096: 14.2 us (64 x 64: 20.8)
+};
+
+// Estimated time of a shape for a layer's rows (with a partition: of the average
+// expert, whose last tile is half full; of 256 rows, one up to half full takes half
+// the time).
+inline float estimate(const Shape& t, const ProductArgs& a, bool gated) {
+  const float steps = steps_of(a.K) / 2;
+  const float cols = ceilf(strips_of(a.N) * (gated ? 64.f : 32.f) / t.bn);
+  float rows = ceilf(static_cast<float>(a.rows) / t.bm);
+  if (a.offsets) {
+    const float mean = static_cast<float>(a.rows) / a.experts;
+    const float each = mean / t.bm + (t.bm == 256 ? 0.4f : 0.5f);
+    rows = (mean < 1.f ? a.rows : a.experts) * (each > 1.f ? each : 1.f);
+  }
+  const float tiles = rows * cols, slots = 256.f * t.per_cu;
+  const float whole = floorf(tiles / slots), rest = tiles - whole * slots;
+  float us = whole * (t.round + steps * t.full);
+  if (rest > 0.f) us += t.round + steps * (rest <= 256.f ? t.alone : t.full);
+  return us;
 }
 
 template <bool GATED>
 void product(const ProductArgs& a, hipStream_t s) {
-  const int64_t per = a.offsets ? a.rows / a.experts : a.rows;     // rows of a layer, on average
-  if (per <= 16) return skinny<1, GATED>(a, s);
-  if (per <= 32) return skinny<2, GATED>(a, s);
-#ifndef SX
-#define SX 4
-#endif
-  if (per <= 512) return tiles<128, 256, 2, 4, SX, GATED>(a, s);
-  tiles<256, 256, 2, 4, SX, GATED>(a, s);
+  // up to 16 rows (32 with a partition) the weights are read once, straight into registers
+  const int64_t mean = a.offsets ? a.rows / a.experts : a.rows;
+  if (mean <= 16) return skinny<1, GATED>(a, s);
+  if (a.offsets && mean <= 32) return skinny<2, GATED>(a, s);
+  int best = 0;
+  float least = 0.f;
+  for (int i = 0; i < static_cast<int>(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
+    const float t = estimate(kShapes[i], a, GATED);
+    if (i == 0 || t < least) {
+      best = i;
+      least = t;
+    }
+  }
+  switch (best) {
+    case 0: return tiles<256, GATED>(a, s);
+    case 1: return tiles<128, GATED>(a, s);
+    case 2: return split<64, 128, 2, 2, 1, 3, GATED>(a, s);
+    case 3: return split<64, 128, 2, 2, 2, 3, GATED>(a, s);
+    case 4: return split<64, 64, 2, 1, 4, 2, GATED>(a, s);
+    default: return split<32, 64, 2, 1, 4, 3, GATED>(a, s);
+  }
 }
 
 }  // namespace
@@ -533,7 +862,12 @@ void token_align_rows(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t
   token_align_kernel<<<static_cast<unsigned>(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(x, ldx, n, d, out, ldo);
 }
 
-void token_product(const ProductArgs& a, hipStream_t s) { a.gated ? product<true>(a, s) : product<false>(a, s); }
+void token_product(const ProductArgs& args, hipStream_t s) {
+  ProductArgs a = args;
+  // rows of x that a tile reads, times their pitch: offsets of 32 bits?
+  a.far = (a.order ? a.x_rows : 256) * a.ldx * 2 >= int64_t(1) << 32;
+  a.gated ? product<true>(a, s) : product<false>(a, s);
+}
 
 void token_combine(const CombineArgs& a, hipStream_t s) {
   const int64_t blocks = (a.n * ((a.d + 7) / 8) + 255) / 256;
