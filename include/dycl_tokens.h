@@ -73,8 +73,8 @@ int dycl_op_norm(const void* x, int x_type, int64_t ldx, const void* y, int y_ty
  * expert) pairs by expert.
  *   p = softmax(logits row) (score 0) or sigmoid(logits) (score 1), float32
  *   v = p + bias
- * An expert is closed to a row where its logit is -infinity or NaN, and all
- * are where mask[row] == 0; a logit of +infinity counts as the largest
+ * An expert is closed to a row where its logit is -infinity or NaN, to all
+ * rows where its bias is, and all are closed where mask[row] == 0; a logit of +infinity counts as the largest
  * finite value.  With groups > 1 the experts are `groups` runs of
  * experts / groups; a group's score is the sum of its two largest v of open
  * experts (its one v if one is open), and only the top_groups best groups
