@@ -1,7 +1,9 @@
-"""Build libdycl.so (the C-ABI library with its gfx950 kernels) in-tree.
+"""Build libdycl.so (the C-ABI library with its gfx950 kernels) in-tree, and
+_tokens.so, the Python binding of its token operators.
 
 ``python -m paper_2307_04963_amd.build`` compiles every source under
-``csrc/`` with hipcc for gfx950 and links ``libdycl.so`` next to this file.
+``csrc/`` with hipcc for gfx950 and links ``libdycl.so`` next to this file, then
+``csrc/binding/`` with the host compiler against torch's headers.
 It always recompiles (objects go to ``_build/`` at the repository root).
 No GPU is needed: hipcc cross-compiles.
 """
@@ -19,6 +21,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libdycl.so")
+BINDING = os.path.join(PKG, "_tokens.so")
 BUILD = os.path.join(ROOT, "_build")
 ARCH = "gfx950"
 
@@ -43,12 +46,48 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_binding() -> str:
+    """The binding's object: host code that sees torch's and HIP's headers."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    src = os.path.join(CSRC, "binding", "tokens.cpp")
+    obj = os.path.join(BUILD, "binding_tokens.o")
+    rocm = os.path.dirname(os.path.dirname(hipcc()))
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(rocm, "include")]
+    for inc in cpp_extension.include_paths():
+        cmd += ["-isystem", inc]
+    cmd += ["-c", src, "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    return obj
+
+
+def _link_binding(obj: str) -> None:
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = BINDING + ".tmp"
+    # (torch's libraries are in the process already; the library beside it is found by its own folder)
+    cmd = [os.environ.get("CXX", "g++"), "-shared", "-fPIC", "-o", tmp, obj, "-L" + PKG, "-l:libdycl.so", "-L" + libs, "-lc10", "-lc10_hip",
+           "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BINDING)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.cpp")) + glob.glob(os.path.join(CSRC, "*.hip")))
     workers = min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
     with cf.ThreadPoolExecutor(workers) as ex:
+        binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, srcs))
+        binding_obj = binding.result()
     tmp = OUT + ".tmp"
     cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -62,8 +101,9 @@ def build(verbose: bool = False) -> str:
         os.remove(tmp)
         raise RuntimeError("undefined symbols in the library:\n" + "\n".join(missing[:20]))
     os.replace(tmp, OUT)
+    _link_binding(binding_obj)
     if verbose:
-        print("built", OUT, flush=True)
+        print("built", OUT, "and", BINDING, flush=True)
     return OUT
 
 
