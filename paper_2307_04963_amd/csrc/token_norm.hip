@@ -6,7 +6,8 @@
 // layer norm's variance from the centred values) come from one read.  A
 // workgroup walks over rows with the weights in registers (read for every
 // row they would double the loads), and requests the next row before it
-// reduces the present one.
+// reduces the present one.  Rows at any alignment are read 16 bytes per lane; element
+// by element, 1999 rows of 1003 took twice as long.
 #include "token_dev.hpp"
 
 namespace dycl {
@@ -20,26 +21,23 @@ struct Raw {
   uint4 v[F32 ? 2 : 1];
 };
 
-// VEC: 8 consecutive elements from `i0`, all inside the row or none; else
-// elements i0 + j * T, each checked
-template <bool F32, bool VEC, int T>
+// 8 consecutive elements from `i0` (rows may start at any element); TAIL: a row's
+// last ones are fewer
+template <bool F32, bool TAIL>
 __device__ __forceinline__ Raw<F32> load8(const void* row, int i0, int d) {
   Raw<F32> r;
-  if constexpr (VEC) {
 #pragma unroll
-    for (int q = 0; q < (F32 ? 2 : 1); ++q) r.v[q] = make_uint4(0, 0, 0, 0);
-    if (i0 < d) {
-      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + static_cast<size_t>(i0) * (F32 ? 4 : 2));
+  for (int q = 0; q < (F32 ? 2 : 1); ++q) r.v[q] = make_uint4(0, 0, 0, 0);
+  if (TAIL ? i0 + 8 <= d : i0 < d) {
+    const char* p = static_cast<const char*>(row) + static_cast<size_t>(i0) * (F32 ? 4 : 2);
 #pragma unroll
-      for (int q = 0; q < (F32 ? 2 : 1); ++q) r.v[q] = p[q];
-    }
-  } else {
+    for (int q = 0; q < (F32 ? 2 : 1); ++q) r.v[q] = load16(p + 16 * q);
+  } else if (TAIL && i0 < d) {
     uint32_t e[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int i = i0 + j * T;
       e[j] = 0;
-      if (i < d) e[j] = F32 ? static_cast<const uint32_t*>(row)[i] : static_cast<const uint16_t*>(row)[i];
+      if (i0 + j < d) e[j] = F32 ? static_cast<const uint32_t*>(row)[i0 + j] : static_cast<const uint16_t*>(row)[i0 + j];
     }
     if constexpr (F32) {
       r.v[0] = make_uint4(e[0], e[1], e[2], e[3]);
@@ -67,27 +65,24 @@ __device__ __forceinline__ void unpack8(const Raw<F32>& r, float* f) {
   }
 }
 
-template <bool VEC, int T>
+template <bool TAIL>
 __device__ __forceinline__ void store8(void* row, bool f32, int i0, int d, const float* f) {
-  if constexpr (VEC) {
-    if (i0 >= d) return;
+  if (TAIL ? i0 + 8 <= d : i0 < d) {
     if (f32) {
-      float4* p = reinterpret_cast<float4*>(static_cast<float*>(row) + i0);
-      p[0] = make_float4(f[0], f[1], f[2], f[3]);
-      p[1] = make_float4(f[4], f[5], f[6], f[7]);
+      float* p = static_cast<float*>(row) + i0;
+      store16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+      store16(p + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
     } else {
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + i0) =
-          make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+      store16(static_cast<uint16_t*>(row) + i0, make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])));
     }
-  } else {
+  } else if (TAIL && i0 < d) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int i = i0 + j * T;
-      if (i >= d) continue;
+    for (int j = 0; j < 7; ++j) {
+      if (i0 + j >= d) continue;
       if (f32)
-        static_cast<float*>(row)[i] = f[j];
+        static_cast<float*>(row)[i0 + j] = f[j];
       else
-        static_cast<uint16_t*>(row)[i] = f2bf(f[j]);
+        static_cast<uint16_t*>(row)[i0 + j] = f2bf(f[j]);
     }
   }
 }
@@ -106,7 +101,7 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
   return v;
 }
 
-template <int T, int NV, bool VEC, bool XF, bool YF, bool BIAS>
+template <int T, int NV, bool TAIL, bool XF, bool YF, bool BIAS>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void token_norm_kernel(NormArgs p) {
   constexpr int ROWS = T < 256 ? 256 / T : 1;
   // a reduction's slot is written again two rows later at the earliest, with
@@ -116,25 +111,43 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void token_norm_kernel(NormArgs 
   const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / T;
   const int d = p.d;
-  auto at = [&](int i) { return VEC ? (i * T + t) * 8 : i * 8 * T + t; };
-  auto in = [&](int i, int j) { return VEC ? at(i) < d : at(i) + j * T < d; };
+  auto at = [&](int i) { return (i * T + t) * 8; };
+  auto in = [&](int i, int j) { return TAIL ? at(i) + j < d : at(i) < d; };
 
-  // post's weight and bias with the channel's scale, pre's weight and bias
-  float pw[NV][8], pb[NV][8], qw[NV][8], qb[NV][8];
+  // post's weight and bias with the channel's scale, pre's weight and bias: kept, or
+  // (of the widest rows, which leave no room) read again for every row
+  constexpr bool KEEP = T < 512;
+  constexpr int NW = KEEP ? NV : 1;
+  float pw[NW][8], pb[NW][8], qw[NW][8], qb[NW][8];
+  auto weights = [&](const float* w, int i, float otherwise, float (&out)[8]) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+    for (int j = 0; j < 8; ++j) out[j] = otherwise;
+    if (w) unpack8<true>(load8<true, TAIL>(w, at(i), d), out);
+  };
+  auto post_weights = [&](int i) __attribute__((always_inline)) {
+    const int k = KEEP ? i : 0;
+    float scale[8];
+    weights(p.channel_scale, i, 1.f, scale);
+    weights(p.post_w, i, 1.f, pw[k]);
+    if (BIAS) weights(p.post_b, i, 0.f, pb[k]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int c = VEC ? at(i) + j : at(i) + j * T;
-      const bool ok = in(i, j);
-      const float s = ok && p.channel_scale ? p.channel_scale[c] : 1.f;
-      pw[i][j] = s * (ok && p.post_w ? p.post_w[c] : 1.f);
-      qw[i][j] = ok && p.pre_w ? p.pre_w[c] : 1.f;
-      if (BIAS) {
-        pb[i][j] = s * (ok && p.post_b ? p.post_b[c] : 0.f);
-        qb[i][j] = ok && p.pre_b ? p.pre_b[c] : 0.f;
-      }
+      pw[k][j] *= scale[j];
+      if (BIAS) pb[k][j] *= scale[j];
     }
+  };
+  auto pre_weights = [&](int i) __attribute__((always_inline)) {
+    const int k = KEEP ? i : 0;
+    weights(p.pre_w, i, 1.f, qw[k]);
+    if (BIAS) weights(p.pre_b, i, 0.f, qb[k]);
+  };
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      post_weights(i);
+      pre_weights(i);
+    }
+  }
 
   const float inv_d = 1.0f / static_cast<float>(d);
   Raw<XF> xr[NV];
@@ -145,10 +158,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void token_norm_kernel(NormArgs 
     const char* xp = static_cast<const char*>(p.x) + row * p.ldx * (XF ? 4 : 2);
     const char* yp = static_cast<const char*>(p.y) + row * p.ldy * (YF ? 4 : 2);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) xr[i] = load8<XF, VEC, T>(xp, at(i), d);
+    for (int i = 0; i < NV; ++i) xr[i] = load8<XF, TAIL>(xp, at(i), d);
     if (p.y && rg != 0.f) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) yr[i] = load8<YF, VEC, T>(yp, at(i), d);
+      for (int i = 0; i < NV; ++i) yr[i] = load8<YF, TAIL>(yp, at(i), d);
     }
   };
 
@@ -202,12 +215,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void token_norm_kernel(NormArgs 
         const char* gp = static_cast<const char*>(p.gate) + row * p.ldg * (YF ? 4 : 2);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+          const int k = KEEP ? i : 0;
+          if (!KEEP) post_weights(i);
           float g[8];
-          if (p.gate) unpack8<YF>(load8<YF, VEC, T>(gp, at(i), d), g);
+          if (p.gate) unpack8<YF>(load8<YF, TAIL>(gp, at(i), d), g);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             float v = (z[i][j] - mean) * inv;
-            v = BIAS ? fmaf(v, pw[i][j], pb[i][j]) : v * pw[i][j];
+            v = BIAS ? fmaf(v, pw[k][j], pb[k][j]) : v * pw[k][j];
             if (p.gate) v *= p.gate_act == 0 ? g[j] : (p.gate_act == 1 ? 1.f : g[j]) * sigmoid_fast(g[j]);
             h[i][j] = fmaf(v, gate_of_row, h[i][j]);
           }
@@ -217,7 +232,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void token_norm_kernel(NormArgs 
     if (p.h) {
       char* hp = static_cast<char*>(p.h) + row * p.ldh * (XF ? 4 : 2);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) store8<VEC, T>(hp, XF, at(i), d, h[i]);
+      for (int i = 0; i < NV; ++i) store8<TAIL>(hp, XF, at(i), d, h[i]);
     }
     if (p.u) {
       float mean = 0.f, inv = 1.f;
@@ -243,59 +258,54 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void token_norm_kernel(NormArgs 
       char* up = static_cast<char*>(p.u) + row * p.ldu * (p.u_f32 ? 4 : 2);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
+        const int k = KEEP ? i : 0;
+        if (!KEEP) pre_weights(i);
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float c = (h[i][j] - mean) * inv;
-          v[j] = BIAS ? fmaf(c, qw[i][j], qb[i][j]) : c * qw[i][j];
+          v[j] = BIAS ? fmaf(c, qw[k][j], qb[k][j]) : c * qw[k][j];
         }
-        store8<VEC, T>(up, p.u_f32, at(i), d, v);
+        store8<TAIL>(up, p.u_f32, at(i), d, v);
       }
     }
   }
 }
 
-template <int T, int NV, bool VEC, bool XF, bool YF>
+template <int T, int NV, bool TAIL, bool XF, bool YF>
 void launch(const NormArgs& a, hipStream_t s) {
   constexpr int NT = T < 256 ? 256 : T, ROWS = T < 256 ? 256 / T : 1;
   const int64_t blocks = (a.n + ROWS - 1) / ROWS;
-  const int most = 256 * (T == 1024 ? 2 : 6);
+  const int most = 256 * (T >= 512 ? 2 : 6);
   const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
   if (a.post_b || a.pre_b)
-    token_norm_kernel<T, NV, VEC, XF, YF, true><<<grid, NT, 0, s>>>(a);
+    token_norm_kernel<T, NV, TAIL, XF, YF, true><<<grid, NT, 0, s>>>(a);
   else
-    token_norm_kernel<T, NV, VEC, XF, YF, false><<<grid, NT, 0, s>>>(a);
+    token_norm_kernel<T, NV, TAIL, XF, YF, false><<<grid, NT, 0, s>>>(a);
 }
 
-template <int T, int NV, bool VEC>
+template <int T, int NV, bool TAIL>
 void by_type(const NormArgs& a, hipStream_t s) {
   if (a.x_f32)
-    a.y_f32 ? launch<T, NV, VEC, true, true>(a, s) : launch<T, NV, VEC, true, false>(a, s);
+    a.y_f32 ? launch<T, NV, TAIL, true, true>(a, s) : launch<T, NV, TAIL, true, false>(a, s);
   else
-    a.y_f32 ? launch<T, NV, VEC, false, true>(a, s) : launch<T, NV, VEC, false, false>(a, s);
+    a.y_f32 ? launch<T, NV, TAIL, false, true>(a, s) : launch<T, NV, TAIL, false, false>(a, s);
 }
 
-template <bool VEC>
+template <bool TAIL>
 void by_size(const NormArgs& a, hipStream_t s) {
-  if (a.d <= 512) return by_type<64, 1, VEC>(a, s);
-  if (a.d <= 1024) return by_type<64, 2, VEC>(a, s);
-  if (a.d <= 2048) return by_type<256, 1, VEC>(a, s);
-  if (a.d <= 4096) return by_type<256, 2, VEC>(a, s);
-  if (a.d <= 8192) return by_type<256, 4, VEC>(a, s);
-  if (a.d <= 16384) return by_type<1024, 2, VEC>(a, s);
-  by_type<1024, 4, VEC>(a, s);
+  if (a.d <= 512) return by_type<64, 1, TAIL>(a, s);
+  if (a.d <= 1024) return by_type<64, 2, TAIL>(a, s);
+  if (a.d <= 2048) return by_type<256, 1, TAIL>(a, s);
+  if (a.d <= 4096) return by_type<256, 2, TAIL>(a, s);
+  if (a.d <= 8192) return by_type<256, 4, TAIL>(a, s);
+  if (a.d <= 16384) return by_type<512, 4, TAIL>(a, s);
+  by_type<1024, 4, TAIL>(a, s);
 }
 
 }  // namespace
 
-void token_norm(const NormArgs& a, hipStream_t s) {
-  auto aligned = [](const void* q, int64_t ld, bool f32) {
-    return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * (f32 ? 4 : 2) % 16 == 0);
-  };
-  const bool vec = a.d % 8 == 0 && aligned(a.x, a.ldx, a.x_f32) && aligned(a.y, a.ldy, a.y_f32) &&
-                   aligned(a.gate, a.ldg, a.y_f32) && aligned(a.h, a.ldh, a.x_f32) && aligned(a.u, a.ldu, a.u_f32);
-  vec ? by_size<true>(a, s) : by_size<false>(a, s);
-}
+void token_norm(const NormArgs& a, hipStream_t s) { a.d % 8 ? by_size<true>(a, s) : by_size<false>(a, s); }
 
 }  // namespace k
 }  // namespace dycl

@@ -58,17 +58,20 @@ __global__ __launch_bounds__(256) void token_align_kernel(const uint16_t* x, int
     const int64_t row = q / per;
     const int c = static_cast<int>(q - row * per) * 8;
     const uint16_t* src = x + row * ldx + c;
-    uint32_t v[8];
+    uint4 v;
+    if (c + 8 <= d) {
+      v = load16(src);
+    } else {
+      uint32_t e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < d ? src[j] : 0;
-    reinterpret_cast<uint4*>(out + row * ldo)[c / 8] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+      for (int j = 0; j < 8; ++j) e[j] = c + j < d ? src[j] : 0;
+      v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    }
+    reinterpret_cast<uint4*>(out + row * ldo)[c / 8] = v;
   }
 }
 
 // ---- tiles ---------------------------------------------------------------------
-
-// the same value in every lane, in a scalar register
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // Rows [row0, row0 + rows) of the product, all of one layer.
 struct Tile {
@@ -77,9 +80,19 @@ struct Tile {
   int rows;
 };
 
+// The tile that `found`'s first lane holds: expert e0 + lane with rows [lo, hi) and
+// `incl` tiles up to its last, t of which (counted alike) is the one.
+__device__ __forceinline__ void take_tile(int lo, int hi, int incl, int e0, int t, uint64_t found, int bm, Tile& out) {
+  const int from = __ffsll(static_cast<unsigned long long>(found)) - 1;
+  const int first = __builtin_amdgcn_readlane(lo, from), end = __builtin_amdgcn_readlane(hi, from);
+  const int last = first + (t - __builtin_amdgcn_readlane(incl, from) + (end - first + bm - 1) / bm) * bm;
+  out.expert = e0 + from;
+  out.row0 = last;
+  out.rows = end - last < bm ? end - last : bm;
+}
+
 // Row tile `t` of `bm` rows: expert after expert.  False past the last one.
-// Every wave finds it for itself.  `total` receives the number of tiles if
-// `count_all`.
+// Every wave finds it for itself.
 __device__ __forceinline__ bool find_tile(const ProductArgs& p, int bm, int64_t t, Tile& out) {
   if (!p.offsets) {
     out.expert = 0;
@@ -93,24 +106,13 @@ __device__ __forceinline__ bool find_tile(const ProductArgs& p, int bm, int64_t 
   for (int e0 = 0; e0 < p.experts; e0 += 64) {
     const int e = e0 + lane;
     const int lo = e < p.experts ? p.offsets[e] : 0, hi = e < p.experts ? p.offsets[e + 1] : 0;
-    const int tiles = (hi - lo + bm - 1) / bm;
-    int incl = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(incl, o);
-      if (lane >= o) incl += u;
-    }
+    const int incl = scan_lanes((hi - lo + bm - 1) / bm);
     const uint64_t found = __ballot(t < before + incl);
     if (found) {
-      const int from = __ffsll(static_cast<unsigned long long>(found)) - 1;
-      const int in = static_cast<int>(t - before) - uniform(__shfl(incl, from) - __shfl(tiles, from));
-      const int first = uniform(__shfl(lo, from)) + in * bm, end = uniform(__shfl(hi, from));
-      out.expert = e0 + from;
-      out.row0 = first;
-      out.rows = end - first < bm ? end - first : bm;
+      take_tile(lo, hi, incl, e0, static_cast<int>(t - before), found, bm, out);
       return true;
     }
-    before += uniform(__shfl(incl, 63));
+    before += __builtin_amdgcn_readlane(incl, 63);
   }
   return false;
 }
@@ -124,16 +126,16 @@ constexpr int kGroup = 8;
 
 __device__ __forceinline__ bool tile_of(const ProductArgs& p, int bm, int col_tiles, Tile& out, int& col) {
   int64_t row_tiles = (p.rows + bm - 1) / bm;
+  int lo = 0, hi = 0, incl = 0;                     // up to 64 experts: one scan for both uses
+  const int lane = threadIdx.x & 63;
   if (p.offsets) {
     row_tiles = 0;
-    const int lane = threadIdx.x & 63;
     for (int e0 = 0; e0 < p.experts; e0 += 64) {
       const int e = e0 + lane;
-      const int rows = e < p.experts ? p.offsets[e + 1] - p.offsets[e] : 0;
-      int tiles = (rows + bm - 1) / bm;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) tiles += __shfl_xor(tiles, o);
-      row_tiles += uniform(tiles);
+      lo = e < p.experts ? p.offsets[e] : 0;
+      hi = e < p.experts ? p.offsets[e + 1] : 0;
+      incl = scan_lanes((hi - lo + bm - 1) / bm);
+      row_tiles += __builtin_amdgcn_readlane(incl, 63);
     }
   }
   const int64_t all = row_tiles * col_tiles, each = all >> 3;
@@ -145,7 +147,10 @@ __device__ __forceinline__ bool tile_of(const ProductArgs& p, int bm, int col_ti
   const int64_t left = row_tiles - group * kGroup;
   const int height = left < kGroup ? static_cast<int>(left) : kGroup;
   col = in / height;
-  return find_tile(p, bm, group * kGroup + (in - col * height), out);
+  const int64_t row_tile = group * kGroup + (in - col * height);
+  if (!p.offsets || p.experts > 64) return find_tile(p, bm, row_tile, out);
+  take_tile(lo, hi, incl, 0, static_cast<int>(row_tile), __ballot(row_tile < incl), bm, out);
+  return true;
 }
 
 __device__ __forceinline__ int64_t source_row(const ProductArgs& p, int64_t row) {
@@ -233,8 +238,8 @@ __device__ __forceinline__ void finish8(const ProductArgs& p, int64_t row, int o
   }
   if (p.residual) {
     const uint16_t* r = p.residual + row * p.ldr + o;
-    if (o + 8 <= p.N && reinterpret_cast<uintptr_t>(r) % 16 == 0) {
-      const uint4 q = *reinterpret_cast<const uint4*>(r);
+    if (o + 8 <= p.N) {
+      const uint4 q = load16(r);
       const uint32_t e[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -258,9 +263,9 @@ __device__ __forceinline__ void store8(const ProductArgs& p, int64_t row, int o,
   const bool whole = o + 8 <= p.N_store;
   if (p.y_kind == Y_F32) {
     float* y = static_cast<float*>(p.y) + row * p.ldy + o;
-    if (whole && reinterpret_cast<uintptr_t>(y) % 16 == 0) {
-      reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(y)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    if (whole) {
+      store16(y, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+      store16(y + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -271,8 +276,8 @@ __device__ __forceinline__ void store8(const ProductArgs& p, int64_t row, int o,
   uint16_t* y = static_cast<uint16_t*>(p.y) + row * p.ldy + o;
   if (p.y_kind == Y_SHARED) {                       // (rows padded to whole strips)
     *reinterpret_cast<uint4*>(y) = pack_shared(v);
-  } else if (whole && reinterpret_cast<uintptr_t>(y) % 16 == 0) {
-    *reinterpret_cast<uint4*>(y) = pack8(v);
+  } else if (whole) {
+    store16(y, pack8(v));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -711,8 +716,8 @@ __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
     const bool whole = o + 8 <= p.d;
     if (p.residual) {
       const uint16_t* r = p.residual + row * p.ldr + o;
-      if (whole && reinterpret_cast<uintptr_t>(r) % 16 == 0) {
-        const uint4 f = *reinterpret_cast<const uint4*>(r);
+      if (whole) {
+        const uint4 f = load16(r);
         const uint32_t e[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -743,8 +748,8 @@ __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
         if (slot[j] >= 0) add_shared(f[j], w[j], v);
     }
     uint16_t* out = p.out + row * p.ldo + o;
-    if (whole && reinterpret_cast<uintptr_t>(out) % 16 == 0) {
-      *reinterpret_cast<uint4*>(out) = pack8(v);
+    if (whole) {
+      store16(out, pack8(v));
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)

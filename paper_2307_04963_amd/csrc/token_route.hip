@@ -46,34 +46,11 @@ __device__ __forceinline__ float wave_max(float v) {
   return lane_value(v, 63);
 }
 
-// exp(x) for x >= -150 (below: exp(-150) = 0): the rounding of x log2(e) is added
-// back, so the result is within two units in the last place
-__device__ __forceinline__ float exp_exact(float x) {
-  x = fmaxf(x, -150.0f);
-  const float h = x * 1.44269502f;
-  const float l = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269502f, -h));
-  const float e = __builtin_amdgcn_exp2f(h);
-  return fmaf(e, l * 0.693147182f, e);
-}
+// exp(x): relative error 2^-24 |x| + one unit, which for the scores that take part in
+// a choice is the rounding of the logit
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-__device__ __forceinline__ float sigmoid_exact(float x) {
-  // (past 3e38 exp2 is infinite and its correction NaN)
-  const float y = fmaxf(fminf(-x, 150.0f), -150.0f), h = y * 1.44269502f;
-  const float l = fmaf(y, 1.92596299e-8f, fmaf(y, 1.44269502f, -h));
-  const float e = __builtin_amdgcn_exp2f(h);
-  return e < 3e38f ? __builtin_amdgcn_rcpf(1.0f + fmaf(e, l * 0.693147182f, e)) : 0.0f;
-}
-
-// inclusive prefix sum over the lanes of a wave
-__device__ __forceinline__ int wave_scan(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o);
-    if (lane >= o) v += u;
-  }
-  return v;
-}
+__device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }
 
 // exclusive prefix sums of `count(e)` over the experts into base[0 .. E], by one wave
 template <class F>
@@ -83,9 +60,9 @@ __device__ __forceinline__ void scan_experts(int E, int* base, F count) {
   for (int e0 = 0; e0 < E; e0 += 64) {
     const int e = e0 + lane;
     const int c = e < E ? count(e) : 0;
-    const int incl = wave_scan(c);
+    const int incl = scan_lanes(c);
     if (e < E) base[e] = total + incl - c;
-    total += __shfl(incl, 63);
+    total += __builtin_amdgcn_readlane(incl, 63);
   }
   if (lane == 0) base[E] = total;
 }
@@ -144,12 +121,12 @@ __device__ __forceinline__ void choose(const RouteArgs& p, const Layout& l, cons
     if (top == kClosed) return;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum += exp_exact(v[i] - top) * (v[i] > kClosed ? 1.f : 0.f);
+    for (int i = 0; i < V; ++i) sum += exp_of(v[i] - top);
     inv = 1.0f / wave_sum(sum);
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const float prob = p.sigmoid ? sigmoid_exact(v[i]) : exp_exact(v[i] - top) * inv;
+    const float prob = p.sigmoid ? sigmoid_of(v[i]) : exp_of(v[i] - top) * inv;
     if (i < l.count) scores[l.first + i] = prob;
     const float s = prob + bias[i];
     v[i] = v[i] > kClosed && s > kClosed ? s : kClosed;
@@ -243,12 +220,12 @@ __device__ __forceinline__ void choose(const RouteArgs& p, const Layout& l, cons
   weight *= p.scale;
 }
 
-// Places the pairs of rows [row0, row0 + rows): masks[e] has a bit for each of
-// them that chose e, base[e] is the position of the first.
-__device__ __forceinline__ void place(const RouteArgs& p, int64_t row0, int rows, const unsigned long long* masks, const int* base) {
+// Places the pairs of rows [row0, row0 + rows), whose choices are `ids`: masks[e] has
+// a bit for each of them that chose e, base[e] is the position of the first.
+__device__ __forceinline__ void place(const RouteArgs& p, const int32_t* ids, int64_t row0, int rows, const unsigned long long* masks, const int* base) {
   for (int q = threadIdx.x; q < rows * p.k; q += blockDim.x) {
     const int64_t pair = row0 * p.k + q;
-    const int e = p.ids[pair];
+    const int e = ids[q];
     int pos = -1;
     if (e >= 0) {
       const int r = q / p.k;
@@ -270,6 +247,7 @@ __global__ __launch_bounds__(V < 16 ? 1024 : 512) void route_choose_kernel(Route
   int* base = reinterpret_cast<int*>(masks + p.experts);
   const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   float* scores = reinterpret_cast<float*>(base + p.experts + 1) + wave * p.experts;
+  int32_t* chosen = reinterpret_cast<int32_t*>(base + p.experts + 1) + waves * p.experts;     // one block: [64][k]
   const Layout l = layout_of<V>(p);
   float bias[V];
   uint32_t next[V];
@@ -304,6 +282,7 @@ __global__ __launch_bounds__(V < 16 ? 1024 : 512) void route_choose_kernel(Route
     if (lane < p.k) {
       p.ids[row * p.k + lane] = id;
       p.weights[row * p.k + lane] = w;
+      if (blocks == 1) chosen[r * p.k + lane] = id;
       if (id >= 0) atomicOr(&masks[id], 1ull << r);
     }
   }
@@ -315,10 +294,9 @@ __global__ __launch_bounds__(V < 16 ? 1024 : 512) void route_choose_kernel(Route
     return;
   }
   if (wave == 0) scan_experts(p.experts, base, [&](int e) { return __popcll(masks[e]); });
-  __threadfence_block();
   __syncthreads();
   for (int e = threadIdx.x; e <= p.experts; e += blockDim.x) p.offsets[e] = base[e];
-  place(p, 0, rows, masks, base);
+  place(p, chosen, 0, rows, masks, base);
   for (int64_t q = base[p.experts] + threadIdx.x; q < p.n * p.k; q += blockDim.x) p.order[q] = -1;
 }
 
@@ -331,7 +309,7 @@ __global__ __launch_bounds__(256) void route_sum_kernel(RouteArgs p, int blocks)
   for (int b0 = 0; b0 < blocks; b0 += 256) {
     const int b = b0 + threadIdx.x;
     const int v = b < blocks ? c[b] : 0;
-    const int incl = wave_scan(v);
+    const int incl = scan_lanes(v);
     if (lane == 63) part[wave] = incl;
     __syncthreads();
     int before = total;
@@ -365,7 +343,7 @@ __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs p, int block
   __syncthreads();
   for (int e = threadIdx.x; e < p.experts; e += 256) base[e] += counts_of(p)[static_cast<size_t>(e) * blocks + blockIdx.x];
   __syncthreads();
-  place(p, row0, rows, masks, base);
+  place(p, p.ids + row0 * p.k, row0, rows, masks, base);
   for (int64_t q = all + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; q < p.n * p.k; q += gridDim.x * 256L) p.order[q] = -1;
 }
 
@@ -376,7 +354,8 @@ __global__ void route_empty_kernel(int32_t* offsets, int experts) {
 template <int V>
 void launch_choose(const RouteArgs& a, int blocks, int block_rows, hipStream_t s) {
   const int waves = blocks > 1 || V >= 16 ? 8 : 16;
-  route_choose_kernel<V><<<blocks, 64 * waves, a.experts * 8 + (a.experts + 1) * 4 + waves * a.experts * 4, s>>>(a, blocks, block_rows);
+  const size_t lds = a.experts * 8 + (a.experts + 1) * 4 + waves * a.experts * 4 + (blocks == 1 ? 64 * a.k * 4 : 0);
+  route_choose_kernel<V><<<blocks, 64 * waves, lds, s>>>(a, blocks, block_rows);
 }
 
 }  // namespace
