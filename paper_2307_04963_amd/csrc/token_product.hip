@@ -23,31 +23,46 @@ constexpr int kFrag = 512;                    // elements of one 16 x 32 operand
 
 // ---- weights -----------------------------------------------------------------
 
-__global__ __launch_bounds__(256) void token_pack_kernel(const uint16_t* w, const uint16_t* gate, int n, int k, int strips,
-                                                         int steps, uint16_t* packed, int64_t vectors) {
-  const int nb = gate ? 4 : 2;
-  for (int64_t q = blockIdx.x * 256L + threadIdx.x; q < vectors; q += gridDim.x * 256L) {
-    const int lane = q & 63;
-    int64_t r = q >> 6;
-    const int b = static_cast<int>(r % nb);
-    r /= nb;
-    const int step = static_cast<int>(r % steps);
-    r /= steps;
-    const int strip = static_cast<int>(r % strips);
-    const int64_t e = r / strips;
-    const int row = lane & 15, half = gate ? b >> 1 : b;
-    const int o = strip * kStrip + 8 * (row >> 2) + 4 * half + (row & 3);
-    const int k0 = step * 32 + 8 * (lane >> 4);
-    uint32_t v[8];
+// A workgroup takes 128 inputs of one strip: rows come in runs of 256 bytes, and
+// the blocks leave from LDS as they lie in the packed layout.  (A lane's own 16 bytes
+// of each row, in the blocks' order, took three times as long.)
+template <int P>                              // products: 2 with a gate
+__global__ __launch_bounds__(256) void token_pack_kernel(const uint16_t* w, const uint16_t* gate, int n, int k, int strips, int steps,
+                                                         uint16_t* packed) {
+  constexpr int CH = 16, PITCH = CH + 1;      // 16-byte chunks of a row's 128 inputs
+  __shared__ uint4 rows[P][kStrip][PITCH];
+  const int parts = (steps + 3) / 4;          // (steps of 32 inputs)
+  const int64_t q = blockIdx.x / parts;
+  const int part = static_cast<int>(blockIdx.x - q * parts);
+  const int64_t e = q / strips;
+  const int strip = static_cast<int>(q - e * strips);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0;
-    if (o < n) {
-      const uint16_t* src = (gate && (b & 1) ? gate : w) + (e * n + o) * k;
+  for (int i = threadIdx.x; i < P * kStrip * CH; i += 256) {
+    const int ch = i % CH, r = i / CH % kStrip, which = i / (CH * kStrip);
+    const int o = strip * kStrip + r, c = part * 128 + ch * 8;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (o < n && c < k) {
+      const uint16_t* src = (which ? gate : w) + (e * n + o) * k + c;
+      if (c + 8 <= k) {
+        v = load16(src);
+      } else {
+        uint32_t t[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (k0 + j < k) v[j] = src[k0 + j];
+        for (int j = 0; j < 8; ++j) t[j] = c + j < k ? src[j] : 0;
+        v = make_uint4(t[0] | t[1] << 16, t[2] | t[3] << 16, t[4] | t[5] << 16, t[6] | t[7] << 16);
+      }
     }
-    reinterpret_cast<uint4*>(packed)[q] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    rows[which][r][ch] = v;
+  }
+  __syncthreads();
+  const int left = steps - part * 4 < 4 ? steps - part * 4 : 4;
+  uint4* out = reinterpret_cast<uint4*>(packed) + ((e * strips + strip) * steps + part * 4) * (2 * P * 64);
+#pragma unroll
+  for (int i = threadIdx.x; i < 4 * 2 * P * 64; i += 256) {
+    const int lane = i % 64, b = i / 64 % (2 * P), step = i / (128 * P);
+    if (step >= left) continue;
+    const int row = lane & 15, half = P == 2 ? b >> 1 : b, which = P == 2 ? b & 1 : 0;
+    out[i] = rows[which][8 * (row >> 2) + 4 * half + (row & 3)][step * 4 + (lane >> 4)];
   }
 }
 
@@ -831,9 +846,14 @@ inline float estimate(const Shape& t, const ProductArgs& a, bool gated) {
 
 template <bool GATED>
 void product(const ProductArgs& a, hipStream_t s) {
-  // up to 16 rows (32 with a partition) the weights are read once, straight into registers
+  // Few rows: the weights go straight into registers, once per 16 rows (of one layer
+  // that is up to 32 rows, from L2 the second time, and 64 of small weights: 32 x 2048 x
+  // 2048 6.3 us against 8.2 in the smallest tiles, 64 x 1024 x 1024 5.7 against 6.4, but 64
+  // x 4096 x 4096 16 against 13), or once per 32 of an expert (333 rows of 32 x 2 experts:
+  // 87 us, 64 x 128 tiles 92).
   const int64_t mean = a.offsets ? a.rows / a.experts : a.rows;
-  if (mean <= 16) return skinny<1, GATED>(a, s);
+  const bool small = static_cast<int64_t>(a.N) * a.K * (GATED ? 2 : 1) <= 1 << 21;
+  if (mean <= 16 || (!a.offsets && mean <= (small ? 64 : 32))) return skinny<1, GATED>(a, s);
   if (a.offsets && mean <= 32) return skinny<2, GATED>(a, s);
   int best = 0;
   float least = 0.f;
@@ -857,9 +877,12 @@ void product(const ProductArgs& a, hipStream_t s) {
 }  // namespace
 
 void token_pack(const uint16_t* w, const uint16_t* gate, int experts, int n, int k, uint16_t* packed, hipStream_t s) {
-  const int64_t vectors = static_cast<int64_t>(packed_elements(experts, n, k, gate != nullptr) / 8);
-  const int64_t blocks = (vectors + 255) / 256;
-  token_pack_kernel<<<static_cast<unsigned>(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(w, gate, n, k, strips_of(n), steps_of(k), packed, vectors);
+  const int strips = strips_of(n), steps = steps_of(k);
+  const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(experts) * strips * ((steps + 3) / 4));
+  if (gate)
+    token_pack_kernel<2><<<blocks, 256, 0, s>>>(w, gate, n, k, strips, steps, packed);
+  else
+    token_pack_kernel<1><<<blocks, 256, 0, s>>>(w, gate, n, k, strips, steps, packed);
 }
 
 void token_align_rows(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t* out, int64_t ldo, hipStream_t s) {
