@@ -355,9 +355,10 @@ __device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& 
 // A workgroup takes one strip of 32 outputs for up to 16 TB rows of one layer;
 // its waves take a range of the K steps each and add their sums through LDS.  Bound by
 // HBM, the weights read once: 5 x 4096 x 4096, 34 MB in 7 to 9 us; one row through
-// eight experts 2048 -> 2 x 1024 -> 2048, 101 MB in 13 + 7 us = 5 TB/s; 333 rows of
-// 2 of 32 experts 1024 -> 2048 -> 1024, 268 MB in 47 to 55 us.  Twice as many steps in
-// flight brought nothing.
+// eight experts 2048 -> 2 x 1024 -> 2048, 101 MB in 13 + 7 us = 5 TB/s; 333 rows
+// crowded on about half of 32 experts, 1024 -> 2048 -> 1024, 170 MB in 21 + 23 us = 3.9
+// TB/s (a crowded expert's weights come again, from L2, for every 32 rows).  Twice as
+// many steps in flight brought nothing.
 template <int TB, bool GATED, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p, int strips, int steps) {
   constexpr int NB = GATED ? 4 : 2, ACC = TB * NB;
