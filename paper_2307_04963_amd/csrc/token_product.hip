@@ -840,7 +840,7 @@ struct Shape {
   float alone, full, round;
 };
 constexpr Shape kShapes[] = {
-    {256, 256, 1, 1.13f, 1.42f, 9.5f},    // 8192 x 8192 x 8192: 787 us (128 x 256: 921)
+    {256, 256, 1, 1.13f, 1.42f, 9.5f},    // 8192 x 8192 x 8192: 764 us (128 x 256: 900)
     {128, 256, 2, 0.75f, 1.50f, 7.0f},    // 16384 x 1024 x 2048: 60 us (256 x 256: 64, 64 x 128: 91)
     {64, 128, 2, 0.36f, 0.58f, 3.5f},     // 1024 x 4096 x 4096: 41 us (128 x 256: 51)
     {64, 128, 1, 0.285f, 0.31f, 3.7f},    // two K groups; 300 x 4096 x 4096: 24.2 us (without: 28.3)
@@ -850,9 +850,11 @@ constexpr Shape kShapes[] = {
 
 // Estimated time of a shape for a layer's rows (with a partition: of the average
 // expert, whose last tile is half full; of 256 rows, one up to half full takes half
-// the time).
+// the time).  Experts' weights come from beyond the L2, which costs steps of 256 rows 7%
+// and smaller ones 14%: 8192 rows of 8 of 64 experts, 2048 -> 2 x 1024 -> 2048, 925 us with
+// the first product in 256 x 256 tiles, 950 with both in 128 x 256, 943 in 256 x 256.
 inline float estimate(const Shape& t, const ProductArgs& a, bool gated) {
-  const float steps = steps_of(a.K) / 2;
+  const float steps = steps_of(a.K) / 2 * (!a.offsets ? 1.f : t.bm == 256 ? 1.07f : 1.14f);
   const float cols = ceilf(strips_of(a.N) * (gated ? 64.f : 32.f) / t.bn);
   float rows = ceilf(static_cast<float>(a.rows) / t.bm);
   if (a.offsets) {
