@@ -320,7 +320,8 @@ __device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& 
   constexpr int NB = GATED ? 4 : 2;
   const int lane = threadIdx.x & 63;
   // strip after strip of a row, so that a wave's two pieces of a line leave together:
-  // 8192 rows of 8 of 64 experts 919 us in 256 x 256 tiles, row after row of a strip 940
+  // 8192 rows of 8 of 64 experts 919 us in 256 x 256 tiles and 277 MB written by the second
+  // product; row after row of a strip 940 and 348
   auto finish = [&](auto act) __attribute__((always_inline)) {
     constexpr int C = RB / NB;
     const int o0 = strip * kStrip + 8 * (lane >> 4);
@@ -587,10 +588,10 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const Tile& t
 // rows or fewer, takes half the time.  128 x 256 tiles on three stages leave room for two
 // workgroups, one's epilogue beside the other's products: better for short K.
 //
-// Measured: gated 8192 x 4096 x 4096 405 us = 1.36 PF, matrix cores 71% busy at the
+// Measured: gated 8192 x 4096 x 4096 398 us = 1.38 PF, matrix cores 73% busy at the
 // clock that the power limit leaves (1.8 to 1.95 GHz); a library's product of that size
-// reaches 1.5 PF.  8192 rows of 8 of 64 experts: 2048 -> 2 x 1024 in 580 us (0.95 PF; 2.6
-// GB pass the L2s for 0.8 GB of rows and weights), 1024 -> 2048 in 365 us (0.75 PF).  Slower:
+// reaches 1.5 PF.  8192 rows of 8 of 64 experts: 2048 -> 2 x 1024 in 560 us (0.98 PF; 2.2
+// GB pass the L2s for 0.8 GB of rows and weights), 1024 -> 2048 in 337 us (0.82 PF).  Slower:
 // matrix instructions of 32 x 32 results (9%), four waves of 128 x 128 (14%), all waves
 // in step (4%).
 template <int BM, bool GATED>
