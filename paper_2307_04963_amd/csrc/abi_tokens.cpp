@@ -28,11 +28,6 @@ bool type_ok(int t) { return t == DYCL_BF16 || t == DYCL_F32; }
 
 size_t size_of(int t) { return t == DYCL_F32 ? 4 : 2; }
 
-void launched(const char* op) {
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) throw dycl::HipError(std::string(op) + ": launch failed: " + hipGetErrorString(e));
-}
-
 size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 
 bool rows_aligned(const uint16_t* x, int64_t ldx, int k) { return at(x, 16) && ldx % 8 == 0 && k % 8 == 0; }
@@ -50,6 +45,17 @@ constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxPitch = int64_t(1) << 40;
 bool pitch_ok(int64_t ld, int64_t width) { return ld >= width && ld < kMaxPitch; }
 
 }  // namespace
+
+namespace dycl {
+namespace k {
+
+void launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) throw HipError(std::string(what) + ": launch failed: " + hipGetErrorString(e));
+}
+
+}  // namespace k
+}  // namespace dycl
 
 extern "C" {
 
@@ -114,7 +120,6 @@ int dycl_op_norm(const void* x, int x_type, int64_t ldx, const void* y, int y_ty
     a.ldh = ldh;
     a.ldu = ldu;
     token_norm(a, static_cast<hipStream_t>(hip_stream));
-    launched(op);
     return static_cast<int>(DYCL_OK);
   });
 }
@@ -145,10 +150,7 @@ int dycl_op_route(const void* logits, int logits_type, int64_t ldl, const float*
          op, "a pointer not aligned to its element");
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (n == 0) {
-      if (offsets) {
-        token_route_empty(offsets, experts, s);
-        launched(op);
-      }
+      if (offsets) token_route_empty(offsets, experts, s);
       return static_cast<int>(DYCL_OK);
     }
     need(logits && ids && weights, op, "null logits, ids or weights");
@@ -176,7 +178,6 @@ int dycl_op_route(const void* logits, int logits_type, int64_t ldl, const float*
     a.slots = slots;
     a.workspace = workspace;
     token_route(a, s);
-    launched(op);
     return static_cast<int>(DYCL_OK);
   });
 }
@@ -194,7 +195,6 @@ int dycl_op_linear_pack(const uint16_t* w, const uint16_t* gate, int experts, in
     need(at(w, 2) && at(gate, 2) && at(packed, 16), op, "a pointer not aligned (packed: 16 bytes)");
     need(packed_bytes >= packed_elements(experts, n, k, gate != nullptr) * 2, op, "output too small");
     token_pack(w, gate, experts, n, k, packed, static_cast<hipStream_t>(hip_stream));
-    launched(op);
     return static_cast<int>(DYCL_OK);
   });
 }
@@ -253,7 +253,6 @@ int dycl_op_linear(const uint16_t* x, int64_t ldx, int64_t m, int k, const uint1
     a.ldy = ldy;
     a.N_store = n;
     token_product(a, s);
-    launched(op);
     return static_cast<int>(DYCL_OK);
   });
 }
@@ -354,7 +353,6 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     c.out = out;
     c.ldo = ldo;
     token_combine(c, s);
-    launched(op);
     return static_cast<int>(DYCL_OK);
   });
 }

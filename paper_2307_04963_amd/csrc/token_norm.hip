@@ -287,6 +287,7 @@ void launch(const NormArgs& a, hipStream_t s) {
     token_norm_kernel<T, NV, TAIL, XF, YF, true><<<grid, NT, 0, s>>>(a);
   else
     token_norm_kernel<T, NV, TAIL, XF, YF, false><<<grid, NT, 0, s>>>(a);
+  launched("norm");
 }
 
 template <int T, int NV, bool TAIL>

@@ -909,11 +909,13 @@ void token_pack(const uint16_t* w, const uint16_t* gate, int experts, int n, int
     token_pack_kernel<2><<<blocks, 256, 0, s>>>(w, gate, n, k, strips, steps, packed);
   else
     token_pack_kernel<1><<<blocks, 256, 0, s>>>(w, gate, n, k, strips, steps, packed);
+  launched("packing");
 }
 
 void token_align_rows(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t* out, int64_t ldo, hipStream_t s) {
   const int64_t blocks = (n * (ldo / 8) + 255) / 256;
   token_align_kernel<<<static_cast<unsigned>(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(x, ldx, n, d, out, ldo);
+  launched("aligned rows");
 }
 
 void token_product(const ProductArgs& args, hipStream_t s) {
@@ -921,11 +923,13 @@ void token_product(const ProductArgs& args, hipStream_t s) {
   // rows of x that a tile reads, times their pitch: offsets of 32 bits?
   a.far = (a.order ? a.x_rows : 256) * a.ldx * 2 >= int64_t(1) << 32;
   a.gated ? product<true>(a, s) : product<false>(a, s);
+  launched("product");
 }
 
 void token_combine(const CombineArgs& a, hipStream_t s) {
   const int64_t blocks = (a.n * ((a.d + 7) / 8) + 255) / 256;
   token_combine_kernel<<<static_cast<unsigned>(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(a);
+  launched("weighted sum");
 }
 
 }  // namespace k

@@ -245,7 +245,7 @@ __device__ __forceinline__ int32_t* counts_of(const RouteArgs& p) { return stati
 
 // (V of 16 and more take more registers than 16 waves leave)
 template <int V>
-__global__ __launch_bounds__(V < 16 ? 1024 : 512) void route_choose_kernel(RouteArgs p, int blocks, int block_rows) {
+__global__ __launch_bounds__(V < 16 ? 1024 : 512) void route_choose_kernel(RouteArgs p, int blocks, int block_rows, int block0) {
   extern __shared__ __align__(16) char lds[];
   unsigned long long* masks = reinterpret_cast<unsigned long long*>(lds);
   int* base = reinterpret_cast<int*>(masks + p.experts);
@@ -257,7 +257,8 @@ __global__ __launch_bounds__(V < 16 ? 1024 : 512) void route_choose_kernel(Route
   uint32_t next[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) bias[i] = i < l.count ? (p.bias ? p.bias[l.first + i] : 0.f) : kClosed;
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * block_rows;
+  const int block = block0 + static_cast<int>(blockIdx.x);
+  const int64_t row0 = static_cast<int64_t>(block) * block_rows;
   const int rows = p.n - row0 < block_rows ? static_cast<int>(p.n - row0) : block_rows;
   // a row's logits are requested a row ahead
   auto request = [&](int r) __attribute__((always_inline)) {
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(V < 16 ? 1024 : 512) void route_choose_kernel(Route
   __syncthreads();
   if (blocks > 1) {
     for (int e = threadIdx.x; e < p.experts; e += blockDim.x)
-      counts_of(p)[static_cast<size_t>(e) * blocks + blockIdx.x] = __popcll(masks[e]);
+      counts_of(p)[static_cast<size_t>(e) * blocks + block] = __popcll(masks[e]);
     return;
   }
   if (wave == 0) scan_experts(p.experts, base, [&](int e) { return __popcll(masks[e]); });
@@ -327,11 +328,12 @@ __global__ __launch_bounds__(256) void route_sum_kernel(RouteArgs p, int blocks)
   if (threadIdx.x == 0) counts_of(p)[static_cast<size_t>(p.experts) * blocks + blockIdx.x] = total;
 }
 
-__global__ __launch_bounds__(256) void route_place_kernel(RouteArgs p, int blocks, int block_rows) {
+__global__ __launch_bounds__(256) void route_place_kernel(RouteArgs p, int blocks, int block_rows, int block0) {
   extern __shared__ __align__(16) char lds[];
   unsigned long long* masks = reinterpret_cast<unsigned long long*>(lds);
   int* base = reinterpret_cast<int*>(masks + p.experts);
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * block_rows;
+  const int block = block0 + static_cast<int>(blockIdx.x);
+  const int64_t row0 = static_cast<int64_t>(block) * block_rows;
   const int rows = p.n - row0 < block_rows ? static_cast<int>(p.n - row0) : block_rows;
   const int32_t* totals = counts_of(p) + static_cast<size_t>(p.experts) * blocks;
   for (int e = threadIdx.x; e < p.experts; e += 256) masks[e] = 0;
@@ -341,25 +343,33 @@ __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs p, int block
     const int e = p.ids[row0 * p.k + q];
     if (e >= 0) atomicOr(&masks[e], 1ull << (q / p.k));
   }
-  if (blockIdx.x == 0)
+  if (block == 0)
     for (int e = threadIdx.x; e <= p.experts; e += 256) p.offsets[e] = base[e];
   const int64_t all = base[p.experts];
   __syncthreads();
-  for (int e = threadIdx.x; e < p.experts; e += 256) base[e] += counts_of(p)[static_cast<size_t>(e) * blocks + blockIdx.x];
+  for (int e = threadIdx.x; e < p.experts; e += 256) base[e] += counts_of(p)[static_cast<size_t>(e) * blocks + block];
   __syncthreads();
   place(p, p.ids + row0 * p.k, row0, rows, masks, base);
-  for (int64_t q = all + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; q < p.n * p.k; q += gridDim.x * 256L) p.order[q] = -1;
+  for (int64_t q = all + static_cast<int64_t>(block) * 256 + threadIdx.x; q < p.n * p.k; q += blocks * 256L) p.order[q] = -1;
 }
 
 __global__ void route_empty_kernel(int32_t* offsets, int experts) {
   for (int e = threadIdx.x; e <= experts; e += blockDim.x) offsets[e] = 0;
 }
 
+// Blocks of one launch.  A launch holds less than 2^32 threads, which 512 threads for
+// every 64 rows pass at 2^29 rows: more blocks take more launches.
+constexpr int kLaunchBlocks = 1 << 22;
+
 template <int V>
 void launch_choose(const RouteArgs& a, int blocks, int block_rows, hipStream_t s) {
   const int waves = blocks > 1 || V >= 16 ? 8 : 16;
   const size_t lds = a.experts * 8 + (a.experts + 1) * 4 + waves * a.experts * 4 + (blocks == 1 ? 64 * a.k * 4 : 0);
-  route_choose_kernel<V><<<blocks, 64 * waves, lds, s>>>(a, blocks, block_rows);
+  for (int b = 0; b < blocks; b += kLaunchBlocks) {
+    const int here = blocks - b < kLaunchBlocks ? blocks - b : kLaunchBlocks;
+    route_choose_kernel<V><<<here, 64 * waves, lds, s>>>(a, blocks, block_rows, b);
+    launched("choice of experts");
+  }
 }
 
 }  // namespace
@@ -389,11 +399,17 @@ void token_route(const RouteArgs& a, hipStream_t s) {
     launch_choose<32>(a, blocks, block_rows, s);
   if (!a.offsets || blocks == 1) return;
   route_sum_kernel<<<a.experts, 256, 0, s>>>(a, blocks);
-  route_place_kernel<<<blocks, 256, a.experts * 8 + (a.experts + 1) * 4, s>>>(a, blocks, block_rows);
+  launched("sums of a partition");
+  for (int b = 0; b < blocks; b += kLaunchBlocks) {
+    const int here = blocks - b < kLaunchBlocks ? blocks - b : kLaunchBlocks;
+    route_place_kernel<<<here, 256, a.experts * 8 + (a.experts + 1) * 4, s>>>(a, blocks, block_rows, b);
+    launched("places of a partition");
+  }
 }
 
 void token_route_empty(int32_t* offsets, int experts, hipStream_t s) {
   route_empty_kernel<<<1, 256, 0, s>>>(offsets, experts);
+  launched("empty partition");
 }
 
 }  // namespace k

@@ -1,6 +1,7 @@
 // Host-side launchers of the token operators' kernels (include/dycl_tokens.h).
-// They check nothing: the C entry points validate every argument before any
-// launch, and each launcher is called with at least one row.
+// They do not check arguments: the C entry points validate every one before any
+// launch, and each launcher is called with at least one row.  Each launch is
+// checked before the next one that reads what it writes.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -10,6 +11,9 @@
 
 namespace dycl {
 namespace k {
+
+// throws HipError if the launch just made was refused
+void launched(const char* what);
 
 struct NormArgs {
   const void *x, *y, *gate;      // [n][d]; y, gate may be null

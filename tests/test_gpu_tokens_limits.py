@@ -1,0 +1,32 @@
+"""The token operators where one launch does not hold all their rows."""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ex():
+    assert torch.cuda.is_available()
+    from paper_2307_04963_amd import experts
+    return experts
+
+
+def test_route_more_rows_than_a_launch_holds(ex):
+    """Blocks of 64 rows by 512 threads: beyond 2^29 rows they are 2^32 threads, more than a launch takes."""
+    n = (1 << 29) + 67
+    print(f"[limits] route n={n}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    z = torch.randint(-3, 4, (n, 2), dtype=torch.int8, device="cuda", generator=g).to(torch.bfloat16)
+    r = ex.route(z, 1)
+    second = z[:, 1] > z[:, 0]                    # equal ones go to the lowest index
+    del z
+    assert torch.equal(r.ids[:, 0], second.int())
+    assert bool((r.weights == 1.0).all())
+    ones = int(second.sum())
+    assert r.offsets.tolist() == [0, n - ones, n]
+    for flags, lo, hi in ((~second, 0, n - ones), (second, n - ones, n)):
+        rows = flags.nonzero()[:, 0].int()
+        assert torch.equal(r.order[lo:hi], rows)
+        assert torch.equal(r.slots[rows.long(), 0], torch.arange(lo, hi, dtype=torch.int32, device="cuda"))
