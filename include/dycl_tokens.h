@@ -141,10 +141,9 @@ int dycl_op_linear(const uint16_t* x, int64_t ldx, int64_t m, int k, const uint1
  *   out[t] = residual[t] + sum over j with slots[t][j] >= 0 of
  *            weights[t][j] * (W2_e f_e(x[t]) + bias2_e),   e the pair's expert
  *   f_e(v) = act(W_e v + bias_e)  or  (W_e v + bias_e) * act(G_e v + gate_bias_e)
- * bf16 in and out; sums, epilogues and the weighted sum are float32; f_e
- * is rounded to bf16 for the second product, and each expert's result is
- * held in 16 bits until it is weighted, off by at most 2^-14 of the largest of
- * eight neighbouring values.
+ * bf16 in and out; sums, epilogues, each expert's results and their weighted
+ * sum are float32.  f_e is rounded to bf16, the second product's input: the
+ * one rounding in between.
  *   x         [n][d] bf16, pitch ldx.
  *   packed1   experts layers of f outputs on d inputs (gated or not),
  *   packed2   experts layers of d outputs on f inputs (not gated), both

@@ -249,7 +249,7 @@ int dycl_op_linear(const uint16_t* x, int64_t ldx, int64_t m, int k, const uint1
     a.residual = residual;
     a.ldr = ldr;
     a.y = y;
-    a.y_kind = y_type == DYCL_F32 ? Y_F32 : Y_BF16;
+    a.y_f32 = y_type == DYCL_F32;
     a.ldy = ldy;
     a.N_store = n;
     token_product(a, s);
@@ -261,7 +261,7 @@ size_t dycl_op_experts_workspace(const uint16_t* x, int64_t ldx, int64_t n, int 
   if (n < 1 || k < 1 || n >= kMaxRows || n * k >= kMaxRows || !layers_ok(experts, d, f)) return 0;
   const size_t pairs = static_cast<size_t>(n) * k;
   const size_t rows = rows_aligned(x, ldx, d) ? 0 : pad256(static_cast<size_t>(n) * round8(d) * 2);
-  return rows + pad256(pairs * strips_of(f) * kStrip * 2) + pad256(pairs * strips_of(d) * kStrip * 2);
+  return rows + pad256(pairs * strips_of(f) * kStrip * 2) + pad256(pairs * strips_of(d) * kStrip * 4);
 }
 
 int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int experts, int k,
@@ -292,8 +292,8 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     char* ws = static_cast<char*>(workspace);
     uint16_t* hidden = reinterpret_cast<uint16_t*>(ws);
     ws += pad256(pairs * fp * 2);
-    uint16_t* part = reinterpret_cast<uint16_t*>(ws);
-    ws += pad256(pairs * dp * 2);
+    float* part = reinterpret_cast<float*>(ws);
+    ws += pad256(pairs * dp * 4);
 
     ProductArgs a{};
     a.x = x;
@@ -335,7 +335,7 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     b.bias = bias2;
     b.act = TACT_NONE;
     b.y = part;
-    b.y_kind = Y_SHARED;
+    b.y_f32 = 1;
     b.ldy = dp;
     b.N_store = static_cast<int>(dp);
     token_product(b, s);

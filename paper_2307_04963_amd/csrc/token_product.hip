@@ -176,58 +176,6 @@ __device__ __forceinline__ int64_t source_row(const ProductArgs& p, int64_t row)
 
 // ---- epilogues -------------------------------------------------------------------
 
-// An expert's results wait for their weighted sum in 16 bits per value: eight
-// consecutive ones share an exponent e, two bits of it above two 15-bit integers
-// q = v 2^(140 - e) 16383 / 16384 in each of four words (the factor keeps a largest
-// value that rounds up within 15 bits).  That is off by 2^-14 of the largest of the
-// eight where bf16 is off by 2^-8 of each value, for the same bytes; float32 would
-// double them.  Exponent 255 marks a group with an infinity or a NaN: it holds the
-// values' upper 15 bits.
-constexpr float kSharedUnit = 16383.0f / 16384.0f;
-
-__device__ __forceinline__ uint4 pack_shared(const float (&v)[8]) {
-  uint32_t m = 0, q[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t u = __float_as_uint(v[j]) & 0x7fffffffu;
-    m = m > u ? m : u;
-  }
-  uint32_t e = m >> 23;                             // (NaN and infinity: 255)
-  if (e < 255) {
-    e = e > 13 ? e : 13;                            // (scale within float32)
-    const float scale = __uint_as_float((267 - e) << 23) * kSharedUnit;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(fmaf(v[j], scale, 12582912.0f));   // 1.5 2^23: rounds to an integer in the low bits
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = (v[j] != v[j] ? 0x7fe00000u : __float_as_uint(v[j])) >> 17;
-  }
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) w[j] = (q[2 * j] & 0x7fff) | (q[2 * j + 1] & 0x7fff) << 15 | (e >> (2 * j)) << 30;
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// sum[j] += weight * value j
-__device__ __forceinline__ void add_shared(const uint4& u, float weight, float (&sum)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-  const int e = w[0] >> 30 | (w[1] >> 30) << 2 | (w[2] >> 30) << 4 | (w[3] >> 30) << 6;
-  if (e != 255) {
-    const float scale = ldexpf(weight * (1.0f / kSharedUnit), e - 140);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      sum[2 * j] = fmaf(scale, static_cast<float>(static_cast<int32_t>(w[j] << 17) >> 17), sum[2 * j]);
-      sum[2 * j + 1] = fmaf(scale, static_cast<float>(static_cast<int32_t>(w[j] << 2) >> 17), sum[2 * j + 1]);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      sum[2 * j] = fmaf(weight, __uint_as_float(w[j] << 17), sum[2 * j]);
-      sum[2 * j + 1] = fmaf(weight, __uint_as_float(w[j] << 2 & 0xfffe0000u), sum[2 * j + 1]);
-    }
-  }
-}
-
 // values [o, o + 8) of an expert's bias vector (0 past the end or without one)
 __device__ __forceinline__ void bias8(const ProductArgs& p, const float* bias, int expert, int o, float (&r)[8]) {
 #pragma unroll
@@ -278,7 +226,7 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
 __device__ __forceinline__ void store8(const ProductArgs& p, int64_t row, int o, const float (&v)[8]) {
   if (o >= p.N_store) return;
   const bool whole = o + 8 <= p.N_store;
-  if (p.y_kind == Y_F32) {
+  if (p.y_f32) {
     float* y = static_cast<float*>(p.y) + row * p.ldy + o;
     if (whole) {
       store16(y, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
@@ -291,9 +239,7 @@ __device__ __forceinline__ void store8(const ProductArgs& p, int64_t row, int o,
     return;
   }
   uint16_t* y = static_cast<uint16_t*>(p.y) + row * p.ldy + o;
-  if (p.y_kind == Y_SHARED) {                       // (rows padded to whole strips)
-    *reinterpret_cast<uint4*>(y) = pack_shared(v);
-  } else if (whole) {
+  if (whole) {
     store16(y, pack8(v));
   } else {
 #pragma unroll
@@ -739,10 +685,10 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void token_split_kernel(ProductA
 
 // ---- the experts' results, weighted and summed ----------------------------------------
 
-// Eight outputs per lane.  A row's slots and weights come first, then up to eight
-// experts' results are requested together: taken one by one, each waited for its
-// slot and then for its values.  Bound by HBM: 8192 rows of 2048, 8 experts each, 336 MB
-// in 61 us = 5.5 TB/s.
+// Eight outputs per lane, float32 until the one rounding of the sum: held in fewer bits,
+// the results' own roundings come to more than the sum's.  A row's slots and weights
+// come first, then up to eight experts' results are requested together: taken one by
+// one, each waited for its slot and then for its values.
 __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
   const int per = (p.d + 7) / 8;
   const int64_t all = p.n * per;
@@ -772,7 +718,7 @@ __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
     for (int j0 = 0; j0 < p.k; j0 += 8) {
       int slot[8];
       float w[8];
-      uint4 f[8];
+      float4 f[8][2];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const bool in = j0 + j < p.k;
@@ -781,10 +727,22 @@ __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (slot[j] >= 0) f[j] = *reinterpret_cast<const uint4*>(p.part + slot[j] * p.ldp + o);
+        if (slot[j] >= 0) {
+          const float4* part = reinterpret_cast<const float4*>(p.part + slot[j] * p.ldp + o);
+          f[j][0] = part[0];
+          f[j][1] = part[1];
+        }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (slot[j] >= 0) add_shared(f[j], w[j], v);
+        if (slot[j] >= 0) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            v[4 * q] = fmaf(w[j], f[j][q].x, v[4 * q]);
+            v[4 * q + 1] = fmaf(w[j], f[j][q].y, v[4 * q + 1]);
+            v[4 * q + 2] = fmaf(w[j], f[j][q].z, v[4 * q + 2]);
+            v[4 * q + 3] = fmaf(w[j], f[j][q].w, v[4 * q + 3]);
+          }
+        }
     }
     uint16_t* out = p.out + row * p.ldo + o;
     if (whole) {

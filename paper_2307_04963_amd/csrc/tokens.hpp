@@ -68,10 +68,6 @@ void token_pack(const uint16_t* w, const uint16_t* gate, int experts, int n, int
 
 enum TokenAct { TACT_NONE = 0, TACT_RELU = 1, TACT_GELU = 2, TACT_SILU = 3 };
 
-// What a product writes: bf16, float32, or an expert's results for
-// token_combine (bf16's size; rows of whole strips, 16-byte aligned).
-enum ProductOut { Y_BF16 = 0, Y_F32 = 1, Y_SHARED = 2 };
-
 // One product over all rows of one layer (offsets null), or over each
 // expert's rows (rows offsets[e] .. offsets[e + 1] - 1 of the layer's output).
 struct ProductArgs {
@@ -92,7 +88,7 @@ struct ProductArgs {
   const uint16_t* residual;
   int64_t ldr;
   void* y;
-  int y_kind;                    // Y_*
+  int y_f32;
   int64_t ldy;
   int N_store;                   // columns written (>= N: the ones past N are 0)
 };
@@ -103,7 +99,7 @@ void token_align_rows(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t
 
 // out[t] = residual[t] + sum_j weights[t][j] * part[slots[t][j]]
 struct CombineArgs {
-  const uint16_t* part;          // rows of pitch ldp, as a product writes them with Y_SHARED
+  const float* part;             // rows of pitch ldp (a multiple of 8), 16-byte aligned
   int64_t ldp;
   const float* weights;
   const int32_t* slots;
