@@ -17,7 +17,9 @@
  * Outputs and workspaces must not overlap inputs or one another, except
  * where said.  Errors are dycl_status codes with dycl_last_error()
  * (dycl.h); validation happens before any launch.  Results do not depend on
- * the order in which workgroups run.
+ * the order in which workgroups run, and a row's results are the same bits
+ * whatever the number and the values of the rows beside it: the number of
+ * rows selects a kernel, never the order of a sum.
  */
 #ifndef DYCL_TOKENS_H_
 #define DYCL_TOKENS_H_

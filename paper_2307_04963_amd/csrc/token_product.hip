@@ -183,10 +183,12 @@ __device__ __forceinline__ void bias8(const ProductArgs& p, const float* bias, i
 }
 
 // Outputs o to o + 7 of one row: bias, activation or gate, residual.  a and b are
-// the strip's blocks, ga and gb the gate's.
+// the strip's blocks, ga and gb the gate's.  (Without fused multiply-adds, which one
+// kernel's instance might get and another's not: a row's bits are the same in all.)
 template <bool GATED, int ACT>
 __device__ __forceinline__ void finish8(const ProductArgs& p, int64_t row, int o, const f32x4& a, const f32x4& b, const f32x4& ga, const f32x4& gb,
                                         const float (&bias)[8], const float (&gate_bias)[8], float (&v)[8]) {
+#pragma clang fp contract(off)
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     v[j] = (j < 4 ? a[j & 3] : b[j & 3]) + bias[j];
@@ -295,96 +297,6 @@ __device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& 
     }
   };
   with_act(p.act, finish);
-}
-
-// ---- few rows per layer: the weights go from memory to the registers --------------
-
-// A workgroup takes one strip of 32 outputs for up to 16 TB rows of one layer;
-// its waves take a range of the K steps each and add their sums through LDS.  Bound by
-// HBM, the weights read once: 5 x 4096 x 4096, 34 MB in 7 to 9 us; one row through
-// eight experts 2048 -> 2 x 1024 -> 2048, 101 MB in 13 + 7 us = 5 TB/s; 333 rows
-// crowded on about half of 32 experts, 1024 -> 2048 -> 1024, 170 MB in 21 + 23 us = 3.9
-// TB/s (a crowded expert's weights come again, from L2, for every 32 rows).  Twice as
-// many steps in flight brought nothing.
-template <int TB, bool GATED, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void token_skinny_kernel(ProductArgs p, int strips, int steps) {
-  constexpr int NB = GATED ? 4 : 2, ACC = TB * NB;
-  constexpr int U = GATED ? 2 : 4;                  // steps whose operands are in flight together
-  __shared__ f32x4 sums[WAVES][ACC][64];
-  Tile tile;
-  const int64_t t = blockIdx.x / strips;
-  const int strip = static_cast<int>(blockIdx.x - t * strips);
-  if (!find_tile(p, 16 * TB, t, tile)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-
-  const uint16_t* xr[TB];
-#pragma unroll
-  for (int b = 0; b < TB; ++b) {
-    const int r = b * 16 + (lane & 15);
-    xr[b] = p.x + source_row(p, tile.row0 + (r < tile.rows ? r : tile.rows - 1)) * p.ldx + 8 * (lane >> 4);
-  }
-  const bf16x8* w = reinterpret_cast<const bf16x8*>(p.w) +
-                    (static_cast<int64_t>(tile.expert) * strips + strip) * steps * (NB * 64) + lane;
-  f32x4 acc[TB][NB];
-#pragma unroll
-  for (int b = 0; b < TB; ++b)
-#pragma unroll
-    for (int c = 0; c < NB; ++c) acc[b][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  const int s0 = wave * steps / WAVES, s1 = (wave + 1) * steps / WAVES;
-  const int k_lane = 8 * (lane >> 4);
-  for (int s = s0; s < s1; s += U) {
-    bf16x8 wf[U][NB], xf[U][TB];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int su = s + u < s1 ? s + u : s1 - 1;
-#pragma unroll
-      for (int c = 0; c < NB; ++c) wf[u][c] = w[(static_cast<int64_t>(su) * NB + c) * 64];
-      const bool in = s + u < s1 && su * 32 + k_lane < p.K;
-#pragma unroll
-      for (int b = 0; b < TB; ++b) {
-        uint4 q = make_uint4(0, 0, 0, 0);
-        if (in) q = *reinterpret_cast<const uint4*>(xr[b] + su * 32);
-        xf[u][b] = __builtin_bit_cast(bf16x8, q);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int b = 0; b < TB; ++b)
-#pragma unroll
-        for (int c = 0; c < NB; ++c)
-          acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[u][c], xf[u][b], acc[b][c], 0, 0, 0);
-  }
-#pragma unroll
-  for (int b = 0; b < TB; ++b)
-#pragma unroll
-    for (int c = 0; c < NB; ++c) sums[wave][b * NB + c][lane] = acc[b][c];
-  __syncthreads();
-  // a wave adds up a block, in the order of the waves; then a wave finishes 16 rows
-  for (int q = wave; q < ACC; q += WAVES) {
-    f32x4 r = sums[0][q][lane];
-#pragma unroll
-    for (int i = 1; i < WAVES; ++i) r += sums[i][q][lane];
-    sums[0][q][lane] = r;
-  }
-  __syncthreads();
-  for (int b = wave; b < TB; b += WAVES) {
-    const int row = b * 16 + (lane & 15);
-    const int o = strip * kStrip + 8 * (lane >> 4);
-    if (row >= tile.rows || o >= p.N_store) continue;
-    float b8[8], g8[8], v[8];
-    bias8(p, p.bias, tile.expert, o, b8);
-    bias8(p, GATED ? p.gate_bias : nullptr, tile.expert, o, g8);
-    const f32x4(&r)[ACC][64] = sums[0];
-    with_act(p.act, [&](auto act) __attribute__((always_inline)) {
-      if (GATED)
-        finish8<true, act>(p, tile.row0 + row, o, r[b * NB][lane], r[b * NB + 2][lane], r[b * NB + 1][lane], r[b * NB + 3][lane], b8, g8, v);
-      else
-        finish8<false, act>(p, tile.row0 + row, o, r[b * NB][lane], r[b * NB + 1][lane], r[b * NB][lane], r[b * NB][lane], b8, g8, v);
-    });
-    store8(p, tile.row0 + row, o, v);
-  }
 }
 
 // ---- many rows: tiles through LDS --------------------------------------------------
@@ -554,133 +466,158 @@ void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
     tile_product<128, 256, 2, 4, S, GATED>(p, tile, col, strips, steps, smem);
 }
 
-// Smaller tiles, for products that large ones would leave CUs idle with: KG groups
-// of WM x WN waves split the K range of one tile (their sums meet in LDS), each with
-// its own ring of S stages of 64 inputs.  A token row of a stage is 128 bytes whose
-// eight 16-byte chunks are stored at chunk ^ (row / 2) % 8.  One barrier per step:
-// behind it, the stage read a step ago takes the loads of step kt + S - 1.
-template <int BM, int BN, int WM, int WN, int KG, int S, bool GATED>
-__global__ __launch_bounds__(64 * WM * WN * KG) void token_split_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
-  constexpr int NT = 64 * WM * WN;                  // threads of a group
-  constexpr int NB = GATED ? 4 : 2;                 // blocks per strip
-  constexpr int WTM = BM / WM, WTN = BN / WN;
-  constexpr int TB = WTM / 16, RB = WTN / 16;
-  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
-  constexpr int JA = BM * 8 / NT, JB = BN * 8 / NT, J = JA + JB;
+// ---- fewer rows: small tiles, a deep ring -------------------------------------------
+
+// BM tokens x BN weight rows, KT times 64 inputs per stage of a ring of S.  Every wave
+// loads, W pieces of 1 KB at a time: eight token rows of 128 bytes, whose eight 16-byte
+// chunks are stored at chunk ^ (row / 2) % 8, or a block of weights.  The first WM x WN
+// waves multiply, each its part of the tile over all steps in order, the order of the
+// large tiles: a row's sums are the same bits whichever kernel takes it.  One barrier
+// per stage: behind it, the stage read a turn ago takes the loads of the stage S - 1 ahead.
+template <int BM, int BN, int WM, int WN, int W, int KT, int S, bool GATED>
+__global__ __launch_bounds__(64 * W) void token_ring_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
+  constexpr int NB = GATED ? 4 : 2;                 // blocks per strip and step
+  constexpr int AU = BM / 8, BU = BN / 8;           // pieces per 64 inputs
+  constexpr int JA = KT * AU / W, JB = KT * BU / W, J = JA + JB;
+  constexpr int CA = AU > W ? AU / W : 1, CB = BU > W ? BU / W : 1;   // of them different ones of a wave
+  constexpr int A_BYTES = BM * 128, PART = A_BYTES + BN * 128, STAGE = KT * PART;
+  constexpr int TB = BM / 16 / WM, RB = BN / 16 / WN;                 // blocks of a wave
   constexpr int TS = BN / 16 / NB;                  // strips per tile
-  static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0 && NT % 128 == 0 && RB % NB == 0 && WTM % 16 == 0, "tile shape");
-  static_assert(S >= 2 && J * (S - 2) < 64 && (KG - 1) * BM * BN * 4 <= KG * S * STAGE, "stages");
-  __shared__ __align__(16) char smem[KG * S * STAGE];
+  static_assert(KT * AU % W == 0 && KT * BU % W == 0 && (W % AU == 0 || AU % W == 0) && (W % BU == 0 || BU % W == 0), "a wave's pieces repeat");
+  static_assert(W % 2 == 0 && AU % 2 == 0, "a wave loads one chunk of its rows");
+  static_assert(WM * WN <= W && TB * WM * 16 == BM && RB * WN * 16 == BN && (RB % NB == 0 || NB % RB == 0), "tile shape");
+  constexpr int PARTS = RB < NB ? NB / RB : 1;      // waves that share a strip
+  static_assert(S >= 2 && J * (S - 2) < 64 && S * STAGE <= 160 * 1024, "stages");
+  __shared__ __align__(16) char smem[S * STAGE];
 
   Tile tile;
   int col;
   if (!tile_of(p, BM, col_tiles, tile, col)) return;
   const int strip0 = col * TS;
-  const int lane = threadIdx.x & 63, tid = threadIdx.x % NT;
-  const int all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = all_wave / (WM * WN), wave = all_wave % (WM * WN);
-  const int wm = wave / WN, wn = wave % WN;
-  char* const ring = smem + group * (S * STAGE);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
+  // this lane's rows of x, as byte offsets, and the K chunk that it loads of each; this wave's blocks of weights
   const uint16_t* const a_base = p.order ? p.x : p.x + tile.row0 * p.ldx;
-  int64_t a_off[JA];
-  const int a_k = ((tid & 7) ^ ((tid >> 4) & 7)) * 8;       // (NT / 8 rows further on, the chunk is the same)
+  // (row / 2 % 8 is the same for all of a wave's pieces: they lie whole times 16 rows apart)
+  const int a_k = ((lane ^ (((wave & 1) << 2) + (lane >> 4))) & 7) * 8;
+  int64_t a_off[CA];
 #pragma unroll
-  for (int j = 0; j < JA; ++j) {
-    const int r = (j * NT + tid) >> 3;
+  for (int j = 0; j < CA; ++j) {
+    const int r = (j * W + wave) % AU * 8 + (lane >> 3);
     const int64_t row = r < tile.rows ? r : tile.rows - 1;
     a_off[j] = ((p.order ? p.order[tile.row0 + row] / p.order_k : row) * p.ldx + a_k) * 2;
   }
   const uint16_t* const b_base = p.w + (static_cast<int64_t>(tile.expert) * strips + strip0) * steps * (NB * kFrag);
-  uint32_t b_off[JB];
+  uint32_t b_off[CB];
 #pragma unroll
-  for (int j = 0; j < JB; ++j) {
-    const int q = (j * NT + tid) >> 6;              // block of the stage
-    int s = q / (2 * NB);
-    s = strip0 + s < strips ? s : strips - 1 - strip0;
-    b_off[j] = (static_cast<uint32_t>(s) * steps * NB + q % (2 * NB)) * (kFrag * 2) + lane * 16;
+  for (int j = 0; j < CB; ++j) {
+    const int c = (j * W + wave) % BU;
+    const int s = strip0 + c / (2 * NB) < strips ? c / (2 * NB) : strips - 1 - strip0;
+    b_off[j] = (static_cast<uint32_t>(s) * steps * NB + c % (2 * NB)) * (kFrag * 2) + lane * 16;
   }
-  const int near = p.far ? 0 : p.K / 64;
-  const int nk_all = steps / 2;
-  const int k0 = group * nk_all / KG, nk = (group + 1) * nk_all / KG - k0;
-  auto load = [&](int kt, char* stage) __attribute__((always_inline)) {
-    if (kt < near) {
+  const int all = steps / 2, near = p.far ? 0 : p.K / 64;   // times 64 inputs: in all, and with all of them at offsets of 32 bits
+  // (those past the last one repeat it: every stage is as many loads)
+  auto load = [&](int i, char* stage) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < JA; ++j) load_lds16(a_base + kt * 64, static_cast<uint32_t>(a_off[j]), stage + (j * NT + wave * 64) * 16);
-    } else {
-#pragma unroll
-      for (int j = 0; j < JA; ++j) {
-        const char* src = reinterpret_cast<const char*>(a_base + kt * 64) + a_off[j];
-        if (kt * 64 + a_k >= p.K) src = reinterpret_cast<const char*>(g_zeros);
-        load_lds16(src, stage + (j * NT + wave * 64) * 16);
+    for (int j = 0; j < JA; ++j) {
+      const int u = j * W + wave, q = u / AU, h0 = i * KT + q, h = h0 < all ? h0 : all - 1;
+      char* const to = stage + q * PART + u % AU * 1024;
+      if (h < near) {
+        load_lds16(a_base + h * 64, static_cast<uint32_t>(a_off[j % CA]), to);
+      } else {
+        const char* src = reinterpret_cast<const char*>(a_base + h * 64) + a_off[j % CA];
+        if (h * 64 + a_k >= p.K) src = reinterpret_cast<const char*>(g_zeros);
+        load_lds16(src, to);
       }
     }
-    const char* const b_step = reinterpret_cast<const char*>(b_base) + static_cast<int64_t>(kt) * (2 * NB * kFrag * 2);
 #pragma unroll
-    for (int j = 0; j < JB; ++j) load_lds16(b_step, b_off[j], stage + A_BYTES + (j * NT + wave * 64) * 16);
+    for (int j = 0; j < JB; ++j) {
+      const int u = j * W + wave, q = u / BU, h0 = i * KT + q, h = h0 < all ? h0 : all - 1;
+      const char* const b_step = reinterpret_cast<const char*>(b_base) + static_cast<int64_t>(h) * (2 * NB * kFrag * 2);
+      load_lds16(b_step, b_off[j % CB], stage + q * PART + A_BYTES + u % BU * 1024);
+    }
   };
-  const int xr = wm * WTM + (lane & 15);
+
+  const int wm = wave / WN, wn = wave % WN;
+  const int xr = wm * (TB * 16) + (lane & 15);
   f32x4 acc[TB][RB];
 #pragma unroll
   for (int b = 0; b < TB; ++b)
 #pragma unroll
     for (int c = 0; c < RB; ++c) acc[b][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const char* part) __attribute__((always_inline)) {
+    bf16x8 x[2][TB], w[2][RB];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int c = 0; c < RB; ++c) {
+        const int blk = wn * RB + c;                // block of the tile: strip blk / NB
+        w[s][c] = *reinterpret_cast<const bf16x8*>(part + A_BYTES + ((blk / NB * 2 + s) * NB + blk % NB) * 1024 + lane * 16);
+      }
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+        x[s][b] = *reinterpret_cast<const bf16x8*>(part + (xr + b * 16) * 128 + (((s * 4 + (lane >> 4)) ^ (xr >> 1)) & 7) * 16);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+#pragma unroll
+        for (int c = 0; c < RB; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[s][c], x[s][b], acc[b][c], 0, 0, 0);
+  };
 
+  const int turns = (all + KT - 1) / KT;
 #pragma unroll
   for (int i = 0; i < S - 1; ++i)
-    if (i < nk) load(k0 + i, ring + i * STAGE);
-  const int turns = (nk_all + KG - 1) / KG;         // of the group with the most steps
-  char* cur = ring;
-  char* prev = ring + (S - 1) * STAGE;
+    if (i < turns) load(i, smem + i * STAGE);
+  char* cur = smem;
+  char* prev = smem + (S - 1) * STAGE;
   for (int i = 0; i < turns; ++i) {
-    if (i + S - 1 <= nk)
+    if (i + S - 1 <= turns)
       wait_all_barrier<J * (S - 2)>();
     else
       wait_all_barrier<0>();
-    if (i + S - 1 < nk) load(k0 + i + S - 1, prev);
-    if (i < nk) {
-      bf16x8 x[2][TB], w[2][RB];
+    if (i + S - 1 < turns) load(i + S - 1, prev);
+    if (wave < WM * WN) {
+      const int left = all - i * KT;
+      if (left >= KT) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int c = 0; c < RB; ++c) {
-          const int blk = wn * RB + c;              // block of the tile: strip blk / NB
-          w[s][c] = *reinterpret_cast<const bf16x8*>(cur + A_BYTES + ((blk / NB * 2 + s) * NB + blk % NB) * 1024 + lane * 16);
-        }
-#pragma unroll
-        for (int b = 0; b < TB; ++b)
-          x[s][b] = *reinterpret_cast<const bf16x8*>(cur + (xr + b * 16) * 128 + (((s * 4 + (lane >> 4)) ^ (xr >> 1)) & 7) * 16);
+        for (int q = 0; q < KT; ++q) multiply(cur + q * PART);
+      } else {
+        for (int q = 0; q < left; ++q) multiply(cur + q * PART);
       }
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int b = 0; b < TB; ++b)
-#pragma unroll
-          for (int c = 0; c < RB; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[s][c], x[s][b], acc[b][c], 0, 0, 0);
     }
     prev = cur;
-    cur = cur == ring + (S - 1) * STAGE ? ring : cur + STAGE;
+    cur = cur == smem + (S - 1) * STAGE ? smem : cur + STAGE;
   }
-
-  if (KG > 1) {
-    // the other groups' sums, in their order
+  if constexpr (PARTS == 1) {
+    if (wave < WM * WN) tile_epilogue<TB, RB, GATED>(p, tile, wm * (TB * 16), strip0 + wn * (RB / NB), acc);
+  } else {
+    // a strip's sums meet in its first wave
     f32x4* const sums = reinterpret_cast<f32x4*>(smem);
+    const int part = wn % PARTS;
     lds_barrier();
-    if (group > 0) {
+    if (wave < WM * WN && part > 0) {
 #pragma unroll
       for (int b = 0; b < TB; ++b)
 #pragma unroll
-        for (int c = 0; c < RB; ++c) sums[(((group - 1) * WM * WN + wave) * TB * RB + b * RB + c) * 64 + lane] = acc[b][c];
+        for (int c = 0; c < RB; ++c) sums[((wave * TB + b) * RB + c) * 64 + lane] = acc[b][c];
     }
     lds_barrier();
-    if (group > 0) return;
-    for (int g = 0; g < KG - 1; ++g)
+    if (wave >= WM * WN || part > 0) return;
+    f32x4 strip[TB][NB];
 #pragma unroll
-      for (int b = 0; b < TB; ++b)
+    for (int b = 0; b < TB; ++b)
 #pragma unroll
-        for (int c = 0; c < RB; ++c) acc[b][c] += sums[((g * WM * WN + wave) * TB * RB + b * RB + c) * 64 + lane];
+      for (int c = 0; c < NB; ++c) {
+        if (c < RB)
+          strip[b][c] = acc[b][c];
+        else
+          strip[b][c] = sums[(((wave + c / RB) * TB + b) * RB + c % RB) * 64 + lane];
+      }
+    tile_epilogue<TB, NB, GATED>(p, tile, wm * (TB * 16), strip0 + wn / PARTS, strip);
   }
-  tile_epilogue<TB, RB, GATED>(p, tile, wm * WTM, strip0 + wn * (RB / NB), acc);
 }
 
 // ---- the experts' results, weighted and summed ----------------------------------------
@@ -763,19 +700,6 @@ int64_t row_tiles(const ProductArgs& a, int bm) {
   return whole + ragged;
 }
 
-template <int TB, bool GATED>
-void skinny(const ProductArgs& a, hipStream_t s) {
-  const int strips = strips_of(a.N), steps = steps_of(a.K);
-  const int64_t groups = row_tiles(a, 16 * TB) * strips;
-  // few workgroups: more waves each, for as many loads in flight
-  if (groups <= 256)
-    token_skinny_kernel<TB, GATED, 16><<<static_cast<unsigned>(groups), 1024, 0, s>>>(a, strips, steps);
-  else if (groups <= 512)
-    token_skinny_kernel<TB, GATED, 8><<<static_cast<unsigned>(groups), 512, 0, s>>>(a, strips, steps);
-  else
-    token_skinny_kernel<TB, GATED, 4><<<static_cast<unsigned>(groups), 256, 0, s>>>(a, strips, steps);
-}
-
 template <int BM, bool GATED>
 void tiles(const ProductArgs& a, hipStream_t s) {
   const int strips = strips_of(a.N), steps = steps_of(a.K), per = 256 / (GATED ? 64 : 32);
@@ -783,28 +707,44 @@ void tiles(const ProductArgs& a, hipStream_t s) {
   token_tile_kernel<BM, GATED><<<static_cast<unsigned>(row_tiles(a, BM) * cols), 512, 0, s>>>(a, strips, steps, cols);
 }
 
-template <int BM, int BN, int WM, int WN, int KG, int S, bool GATED>
-void split(const ProductArgs& a, hipStream_t s) {
+template <int BM, int BN, int WM, int WN, int W, int KT, int S, bool GATED>
+void ring(const ProductArgs& a, hipStream_t s) {
   const int strips = strips_of(a.N), steps = steps_of(a.K), per = BN / (GATED ? 64 : 32);
   const int cols = (strips + per - 1) / per;
-  token_split_kernel<BM, BN, WM, WN, KG, S, GATED>
-      <<<static_cast<unsigned>(row_tiles(a, BM) * cols), 64 * WM * WN * KG, 0, s>>>(a, strips, steps, cols);
+  token_ring_kernel<BM, BN, WM, WN, W, KT, S, GATED><<<static_cast<unsigned>(row_tiles(a, BM) * cols), 64 * W, 0, s>>>(a, strips, steps, cols);
 }
 
 // Which kernel: the one whose estimate is least.  A round of tiles (256 CUs, per_cu
-// workgroups each) takes `round` microseconds and `full` per K step of 64, `alone`
-// where each CU has one; fitted to products of 16 to 16384 rows and K of 128 to 8192.
+// workgroups each) takes `round` microseconds and `full` per 64 inputs, `alone` where
+// each CU has one; fitted to 373 plain and 356 gated products of 16 to 8192 rows, 512
+// to 8192 outputs and 256 to 8192 inputs, their weights from memory: the choice is 0.5% and
+// 0.2% slower there than each product's best.  Leaving a shape out costs 0.2 to 4% on
+// average.  Beside each, us of a product of its own and of the next best without it.
+// (rows x inputs x outputs; gated: two products.)
 struct Shape {
   int bm, bn, per_cu;
   float alone, full, round;
 };
-constexpr Shape kShapes[] = {
-    {256, 256, 1, 1.13f, 1.42f, 9.5f},    // 8192 x 8192 x 8192: 764 us (128 x 256: 900)
-    {128, 256, 2, 0.75f, 1.50f, 7.0f},    // 16384 x 1024 x 2048: 60 us (256 x 256: 64, 64 x 128: 91)
-    {64, 128, 2, 0.36f, 0.58f, 3.5f},     // 1024 x 4096 x 4096: 41 us (128 x 256: 51)
-    {64, 128, 1, 0.285f, 0.31f, 3.7f},    // two K groups; 300 x 4096 x 4096: 24.2 us (without: 28.3)
-    {64, 64, 1, 0.245f, 0.25f, 2.9f},     // four K groups; 512 x 2048 x 2048: 11.9 us (64 x 128: 15.0)
-    {32, 64, 1, 0.135f, 0.14f, 2.5f},     // four K groups; 128 x 4096 x 4096: 14.2 us (64 x 64: 20.8)
+constexpr Shape kPlain[] = {
+    {256, 256, 1, 1.185f, 1.599f, 9.5f},
+    {128, 256, 2, 0.960f, 1.989f, 5.4f},
+    {64, 128, 2, 0.423f, 0.688f, 3.6f},
+    {64, 128, 1, 0.391f, 0.392f, 3.5f},    // 300 x 4096 x 4096: 29.5 (64 x 128, two per CU: 31.6)
+    {64, 64, 1, 0.263f, 0.260f, 3.3f},     // 256 x 4096 x 4096: 20.8 (32 x 64: 30.5)
+    {32, 64, 1, 0.173f, 0.178f, 3.2f},     // 100 x 4096 x 4096: 15.5 (32 x 32: 19.5)
+    {32, 32, 1, 0.115f, 0.118f, 3.2f},     // 48 x 4096 x 4096: 11.9 (32 x 64: 16.0)
+    {16, 32, 1, 0.082f, 0.084f, 3.3f},     // 1 x 4096 x 4096: 10.1 (three per CU: 16.5)
+    {16, 32, 3, 0.144f, 0.221f, 3.0f},     // 4 x 1024 x 20000: 10.3 (one per CU: 14.4)
+};
+constexpr Shape kGated[] = {
+    {256, 256, 1, 1.185f, 1.566f, 8.7f},
+    {128, 256, 2, 0.989f, 1.932f, 5.0f},
+    {64, 128, 2, 0.429f, 0.680f, 3.8f},
+    {64, 128, 1, 0.408f, 0.421f, 3.6f},    // 512 x 2048 x 2048: 16.8 (two per CU: 17.6)
+    {64, 64, 1, 0.276f, 0.285f, 3.6f},     // 256 x 2048 x 2048: 12.9 (32 x 64: 18.7)
+    {32, 64, 1, 0.192f, 0.196f, 3.5f},     // 64 x 4096 x 4096: 19.4 (64 x 64: 23.8)
+    {16, 64, 1, 0.166f, 0.169f, 3.2f},     // 1 x 4096 x 4096: 16.3 (32 x 64: 16.7)
+    {16, 64, 2, 0.210f, 0.286f, 3.2f},     // 16 rows of 8 of 64 experts, 2048 -> 2 x 1024 -> 2048: 130 a call (one per CU: 138)
 };
 
 // Estimated time of a shape for a layer's rows (with a partition: of the average
@@ -828,33 +768,44 @@ inline float estimate(const Shape& t, const ProductArgs& a, bool gated) {
   return us;
 }
 
-template <bool GATED>
-void product(const ProductArgs& a, hipStream_t s) {
-  // Few rows: the weights go straight into registers, once per 16 rows (of one layer
-  // that is up to 32 rows, from L2 the second time, and 64 of small weights: 32 x 2048 x
-  // 2048 6.3 us against 8.2 in the smallest tiles, 64 x 1024 x 1024 5.7 against 6.4, but 64
-  // x 4096 x 4096 16 against 13), or once per 32 of an expert (333 rows of 32 x 2 experts:
-  // 87 us, 64 x 128 tiles 92).
-  const int64_t mean = a.offsets ? a.rows / a.experts : a.rows;
-  const bool small = static_cast<int64_t>(a.N) * a.K * (GATED ? 2 : 1) <= 1 << 21;
-  if (mean <= 16 || (!a.offsets && mean <= (small ? 64 : 32))) return skinny<1, GATED>(a, s);
-  if (a.offsets && mean <= 32) return skinny<2, GATED>(a, s);
+template <size_t C>
+int best_of(const Shape (&shapes)[C], const ProductArgs& a, bool gated) {
   int best = 0;
   float least = 0.f;
-  for (int i = 0; i < static_cast<int>(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
-    const float t = estimate(kShapes[i], a, GATED);
+  for (int i = 0; i < static_cast<int>(C); ++i) {
+    const float t = estimate(shapes[i], a, gated);
     if (i == 0 || t < least) {
       best = i;
       least = t;
     }
   }
-  switch (best) {
-    case 0: return tiles<256, GATED>(a, s);
-    case 1: return tiles<128, GATED>(a, s);
-    case 2: return split<64, 128, 2, 2, 1, 3, GATED>(a, s);
-    case 3: return split<64, 128, 2, 2, 2, 3, GATED>(a, s);
-    case 4: return split<64, 64, 2, 1, 4, 2, GATED>(a, s);
-    default: return split<32, 64, 2, 1, 4, 3, GATED>(a, s);
+  return best;
+}
+
+void plain(const ProductArgs& a, hipStream_t s) {
+  switch (best_of(kPlain, a, false)) {
+    case 0: return tiles<256, false>(a, s);
+    case 1: return tiles<128, false>(a, s);
+    case 2: return ring<64, 128, 2, 4, 8, 1, 3, false>(a, s);
+    case 3: return ring<64, 128, 2, 4, 8, 2, 3, false>(a, s);
+    case 4: return ring<64, 64, 4, 2, 8, 2, 3, false>(a, s);
+    case 5: return ring<32, 64, 2, 2, 8, 4, 3, false>(a, s);
+    case 6: return ring<32, 32, 2, 2, 8, 4, 4, false>(a, s);
+    case 7: return ring<16, 32, 1, 2, 8, 8, 3, false>(a, s);
+    default: return ring<16, 32, 1, 2, 8, 4, 2, false>(a, s);
+  }
+}
+
+void gated(const ProductArgs& a, hipStream_t s) {
+  switch (best_of(kGated, a, true)) {
+    case 0: return tiles<256, true>(a, s);
+    case 1: return tiles<128, true>(a, s);
+    case 2: return ring<64, 128, 2, 2, 8, 1, 3, true>(a, s);
+    case 3: return ring<64, 128, 4, 2, 8, 2, 3, true>(a, s);
+    case 4: return ring<64, 64, 4, 1, 8, 2, 3, true>(a, s);
+    case 5: return ring<32, 64, 2, 2, 8, 4, 3, true>(a, s);
+    case 6: return ring<16, 64, 1, 4, 8, 4, 3, true>(a, s);
+    default: return ring<16, 64, 1, 4, 4, 2, 3, true>(a, s);
   }
 }
 
@@ -880,7 +831,7 @@ void token_product(const ProductArgs& args, hipStream_t s) {
   ProductArgs a = args;
   // rows of x that a tile reads, times their pitch: offsets of 32 bits?
   a.far = (a.order ? a.x_rows : 256) * a.ldx * 2 >= int64_t(1) << 32;
-  a.gated ? product<true>(a, s) : product<false>(a, s);
+  a.gated ? gated(a, s) : plain(a, s);
   launched("product");
 }
 
