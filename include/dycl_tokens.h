@@ -131,8 +131,17 @@ int dycl_op_linear_pack(const uint16_t* w, const uint16_t* gate, int experts, in
  *   workspace dycl_op_linear_workspace(x, ldx, m, k, n, gated) bytes, 16-byte aligned:
  *             0 (NULL) where x is 16-byte aligned and k and ldx are
  *             multiples of 8, room for aligned rows otherwise.
- * m >= 0 (0 does nothing).
+ * m >= 0 (0 does nothing).  A launch holds 2^23 - 1 tiles; more than that of
+ * the largest (256 rows x 256 outputs, 128 gated) return DYCL_E_INVALID, here
+ * and below.
+ *
+ * dycl_op_linear_tile tells which kernel a product takes: tile receives the
+ * rows and outputs of its tiles and how many of them a CU takes together.
+ * experts 0: dycl_op_linear on `rows` rows.  experts > 0: a product of
+ * dycl_op_experts over `rows` pairs (n outputs on k inputs each).  For
+ * profiles and tests; results do not depend on it.
  */
+int dycl_op_linear_tile(int64_t rows, int n, int k, int gated, int experts, int32_t tile[3]);
 size_t dycl_op_linear_workspace(const uint16_t* x, int64_t ldx, int64_t m, int k, int n, int gated);
 int dycl_op_linear(const uint16_t* x, int64_t ldx, int64_t m, int k, const uint16_t* packed, int n, int gated,
                    const float* bias, const float* gate_bias, int act, const uint16_t* residual, int64_t ldr, void* y,

@@ -25,7 +25,7 @@ OPS_EXPORTS = ["dycl_op_compact_workspace", "dycl_op_compact", "dycl_op_compact_
                "dycl_op_conv_pair"]
 # every symbol include/dycl_tokens.h declares
 TOKENS_EXPORTS = ["dycl_op_norm", "dycl_op_route_workspace", "dycl_op_route", "dycl_op_linear_packed_bytes", "dycl_op_linear_pack",
-                  "dycl_op_linear_workspace", "dycl_op_linear", "dycl_op_experts_workspace", "dycl_op_experts"]
+                  "dycl_op_linear_tile", "dycl_op_linear_workspace", "dycl_op_linear", "dycl_op_experts_workspace", "dycl_op_experts"]
 
 
 class DyclError(RuntimeError):
@@ -109,6 +109,8 @@ def _load():
     lib.dycl_op_linear_packed_bytes.restype = sz
     lib.dycl_op_linear_pack.argtypes = [vp, vp, i32, i32, i32, vp, sz, vp]
     lib.dycl_op_linear_pack.restype = i32
+    lib.dycl_op_linear_tile.argtypes = [i64, i32, i32, i32, i32, C.POINTER(i32)]
+    lib.dycl_op_linear_tile.restype = i32
     lib.dycl_op_linear_workspace.argtypes = [vp, i64, i64, i32, i32, i32]
     lib.dycl_op_linear_workspace.restype = sz
     lib.dycl_op_linear.argtypes = [vp, i64, i64, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i32, i64, vp, sz, vp]

@@ -42,6 +42,8 @@ bool layers_ok(int experts, int n, int k) {
 
 constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxPitch = int64_t(1) << 40;
 
+const char* const kTooMany = "more tiles of results than a launch holds";
+
 bool pitch_ok(int64_t ld, int64_t width) { return ld >= width && ld < kMaxPitch; }
 
 }  // namespace
@@ -186,6 +188,27 @@ size_t dycl_op_linear_packed_bytes(int experts, int n, int k, int gated) {
   return layers_ok(experts, n, k) ? packed_elements(experts, n, k, gated) * 2 : 0;
 }
 
+int dycl_op_linear_tile(int64_t rows, int n, int k, int gated, int experts, int32_t tile[3]) {
+  return guarded([&] {
+    const char* op = "dycl_op_linear_tile";
+    need(layers_ok(experts ? experts : 1, n, k), op, "experts outside [0, 1024], or n or k outside [1, 2^20]");
+    need(rows >= 1 && rows < kMaxRows, op, "rows outside [1, 2^31)");
+    need(tile, op, "null tile");
+    ProductArgs a{};
+    const int32_t some = 0;
+    a.offsets = experts ? &some : nullptr;   // (only whether there are any)
+    a.experts = experts ? experts : 1;
+    a.rows = rows;
+    a.K = k;
+    a.N = n;
+    a.gated = gated != 0;
+    const int shape = token_product_shape(a);
+    need(shape >= 0, op, kTooMany);
+    token_product_tile(shape, gated != 0, tile);
+    return static_cast<int>(DYCL_OK);
+  });
+}
+
 int dycl_op_linear_pack(const uint16_t* w, const uint16_t* gate, int experts, int n, int k, uint16_t* packed,
                         size_t packed_bytes, void* hip_stream) {
   return guarded([&] {
@@ -230,12 +253,6 @@ int dycl_op_linear(const uint16_t* x, int64_t ldx, int64_t m, int k, const uint1
     ProductArgs a{};
     a.x = x;
     a.ldx = ldx;
-    if (!rows_aligned(x, ldx, k)) {
-      uint16_t* rows = static_cast<uint16_t*>(workspace);
-      token_align_rows(x, ldx, m, k, rows, round8(k), s);
-      a.x = rows;
-      a.ldx = round8(k);
-    }
     a.order_k = 1;
     a.experts = 1;
     a.rows = m;
@@ -252,7 +269,15 @@ int dycl_op_linear(const uint16_t* x, int64_t ldx, int64_t m, int k, const uint1
     a.y_f32 = y_type == DYCL_F32;
     a.ldy = ldy;
     a.N_store = n;
-    token_product(a, s);
+    const int shape = token_product_shape(a);
+    need(shape >= 0, op, kTooMany);
+    if (!rows_aligned(x, ldx, k)) {
+      uint16_t* rows = static_cast<uint16_t*>(workspace);
+      token_align_rows(x, ldx, m, k, rows, round8(k), s);
+      a.x = rows;
+      a.ldx = round8(k);
+    }
+    token_product(a, shape, s);
     return static_cast<int>(DYCL_OK);
   });
 }
@@ -298,12 +323,6 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     ProductArgs a{};
     a.x = x;
     a.ldx = ldx;
-    if (!rows_aligned(x, ldx, d)) {
-      uint16_t* rows = reinterpret_cast<uint16_t*>(ws);
-      token_align_rows(x, ldx, n, d, rows, round8(d), s);
-      a.x = rows;
-      a.ldx = round8(d);
-    }
     a.order = order;
     a.order_k = k;
     a.x_rows = n;
@@ -320,7 +339,6 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     a.y = hidden;
     a.ldy = fp;
     a.N_store = static_cast<int>(fp);
-    token_product(a, s);
 
     ProductArgs b{};
     b.x = hidden;
@@ -338,7 +356,17 @@ int dycl_op_experts(const uint16_t* x, int64_t ldx, int64_t n, int d, int f, int
     b.y_f32 = 1;
     b.ldy = dp;
     b.N_store = static_cast<int>(dp);
-    token_product(b, s);
+
+    const int first = token_product_shape(a), second = token_product_shape(b);
+    need(first >= 0 && second >= 0, op, kTooMany);
+    if (!rows_aligned(x, ldx, d)) {
+      uint16_t* rows = reinterpret_cast<uint16_t*>(ws);
+      token_align_rows(x, ldx, n, d, rows, round8(d), s);
+      a.x = rows;
+      a.ldx = round8(d);
+    }
+    token_product(a, first, s);
+    token_product(b, second, s);
 
     CombineArgs c{};
     c.part = part;

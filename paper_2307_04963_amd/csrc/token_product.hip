@@ -21,6 +21,9 @@ namespace {
 
 constexpr int kFrag = 512;                    // elements of one 16 x 32 operand block
 
+// A launch holds less than 2^32 threads: of workgroups of up to 512, fewer than this.
+constexpr int64_t kLaunchBlocks = (int64_t(1) << 23) - 1;
+
 // ---- weights -----------------------------------------------------------------
 
 // A workgroup takes 128 inputs of one strip: rows come in runs of 256 bytes, and
@@ -28,12 +31,13 @@ constexpr int kFrag = 512;                    // elements of one 16 x 32 operand
 // of each row, in the blocks' order, took three times as long.)
 template <int P>                              // products: 2 with a gate
 __global__ __launch_bounds__(256) void token_pack_kernel(const uint16_t* w, const uint16_t* gate, int n, int k, int strips, int steps,
-                                                         uint16_t* packed) {
+                                                         int64_t block0, uint16_t* packed) {
   constexpr int CH = 16, PITCH = CH + 1;      // 16-byte chunks of a row's 128 inputs
   __shared__ uint4 rows[P][kStrip][PITCH];
   const int parts = (steps + 3) / 4;          // (steps of 32 inputs)
-  const int64_t q = blockIdx.x / parts;
-  const int part = static_cast<int>(blockIdx.x - q * parts);
+  const int64_t block = block0 + blockIdx.x;
+  const int64_t q = block / parts;
+  const int part = static_cast<int>(block - q * parts);
   const int64_t e = q / strips;
   const int strip = static_cast<int>(q - e * strips);
 #pragma unroll
@@ -770,13 +774,16 @@ inline float estimate(const Shape& t, const ProductArgs& a, bool gated) {
   return us;
 }
 
+// -1 where no shape's tiles are as few as a launch holds
 template <size_t C>
 int best_of(const Shape (&shapes)[C], const ProductArgs& a, bool gated) {
-  int best = 0;
+  int best = -1;
   float least = 0.f;
   for (int i = 0; i < static_cast<int>(C); ++i) {
+    const int64_t cols = (strips_of(a.N) * int64_t(gated ? 64 : 32) + shapes[i].bn - 1) / shapes[i].bn;
+    if (row_tiles(a, shapes[i].bm) * cols >= kLaunchBlocks) continue;
     const float t = estimate(shapes[i], a, gated);
-    if (i == 0 || t < least) {
+    if (best < 0 || t < least) {
       best = i;
       least = t;
     }
@@ -784,8 +791,8 @@ int best_of(const Shape (&shapes)[C], const ProductArgs& a, bool gated) {
   return best;
 }
 
-void plain(const ProductArgs& a, hipStream_t s) {
-  switch (best_of(kPlain, a, false)) {
+void plain(const ProductArgs& a, int shape, hipStream_t s) {
+  switch (shape) {
     case 0: return tiles<256, false>(a, s);
     case 1: return tiles<128, false>(a, s);
     case 2: return ring<64, 128, 2, 4, 8, 1, 3, false>(a, s);
@@ -798,8 +805,8 @@ void plain(const ProductArgs& a, hipStream_t s) {
   }
 }
 
-void gated(const ProductArgs& a, hipStream_t s) {
-  switch (best_of(kGated, a, true)) {
+void gated(const ProductArgs& a, int shape, hipStream_t s) {
+  switch (shape) {
     case 0: return tiles<256, true>(a, s);
     case 1: return tiles<128, true>(a, s);
     case 2: return ring<64, 128, 2, 2, 8, 1, 3, true>(a, s);
@@ -815,12 +822,15 @@ void gated(const ProductArgs& a, hipStream_t s) {
 
 void token_pack(const uint16_t* w, const uint16_t* gate, int experts, int n, int k, uint16_t* packed, hipStream_t s) {
   const int strips = strips_of(n), steps = steps_of(k);
-  const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(experts) * strips * ((steps + 3) / 4));
-  if (gate)
-    token_pack_kernel<2><<<blocks, 256, 0, s>>>(w, gate, n, k, strips, steps, packed);
-  else
-    token_pack_kernel<1><<<blocks, 256, 0, s>>>(w, gate, n, k, strips, steps, packed);
-  launched("packing");
+  const int64_t blocks = static_cast<int64_t>(experts) * strips * ((steps + 3) / 4);
+  for (int64_t b = 0; b < blocks; b += kLaunchBlocks) {
+    const unsigned here = static_cast<unsigned>(blocks - b < kLaunchBlocks ? blocks - b : kLaunchBlocks);
+    if (gate)
+      token_pack_kernel<2><<<here, 256, 0, s>>>(w, gate, n, k, strips, steps, b, packed);
+    else
+      token_pack_kernel<1><<<here, 256, 0, s>>>(w, gate, n, k, strips, steps, b, packed);
+    launched("packing");
+  }
 }
 
 void token_align_rows(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t* out, int64_t ldo, hipStream_t s) {
@@ -829,11 +839,20 @@ void token_align_rows(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t
   launched("aligned rows");
 }
 
-void token_product(const ProductArgs& args, hipStream_t s) {
+int token_product_shape(const ProductArgs& a) { return a.gated ? best_of(kGated, a, true) : best_of(kPlain, a, false); }
+
+void token_product_tile(int shape, bool gated, int tile[3]) {
+  const Shape& t = gated ? kGated[shape] : kPlain[shape];
+  tile[0] = t.bm;
+  tile[1] = gated ? t.bn / 2 : t.bn;
+  tile[2] = t.per_cu;
+}
+
+void token_product(const ProductArgs& args, int shape, hipStream_t s) {
   ProductArgs a = args;
   // rows of x that a tile reads, times their pitch: offsets of 32 bits?
   a.far = (a.order ? a.x_rows : 256) * a.ldx * 2 >= int64_t(1) << 32;
-  a.gated ? gated(a, s) : plain(a, s);
+  a.gated ? gated(a, shape, s) : plain(a, shape, s);
   launched("product");
 }
 

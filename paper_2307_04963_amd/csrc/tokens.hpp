@@ -92,7 +92,12 @@ struct ProductArgs {
   int64_t ldy;
   int N_store;                   // columns written (>= N: the ones past N are 0)
 };
-void token_product(const ProductArgs& a, hipStream_t stream);
+// The shape that a product takes, by its rows, sizes and experts; -1 where none's tiles
+// are as few as a launch holds.
+int token_product_shape(const ProductArgs& a);
+// a shape's rows and outputs per tile, and workgroups per CU
+void token_product_tile(int shape, bool gated, int tile[3]);
+void token_product(const ProductArgs& a, int shape, hipStream_t stream);
 
 // rows [n][d] of any alignment to rows of pitch `ldo` (a multiple of 8), zero-padded
 void token_align_rows(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t* out, int64_t ldo, hipStream_t stream);

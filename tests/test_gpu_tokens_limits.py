@@ -30,3 +30,13 @@ def test_route_more_rows_than_a_launch_holds(ex):
         rows = flags.nonzero()[:, 0].int()
         assert torch.equal(r.order[lo:hi], rows)
         assert torch.equal(r.slots[rows.long(), 0], torch.arange(lo, hi, dtype=torch.int32, device="cuda"))
+
+
+def test_pack_more_than_a_launch_holds(ex):
+    """257 x 2^15 strips of weights: beyond the 2^23 - 1 workgroups of a launch."""
+    print("[limits] pack 257 x 2^20 x 1", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    w = torch.randint(-100, 101, (257, 1 << 20, 1), dtype=torch.int8, device="cuda", generator=g).to(torch.bfloat16)
+    packed = ex.pack(w).data.view(257, -1)
+    for e in (0, 128, 255, 256):
+        assert torch.equal(packed[e], ex.pack(w[e]).data)
