@@ -125,7 +125,7 @@ int dycl_op_linear_pack(const uint16_t* w, const uint16_t* gate, int experts, in
  *   x         [m][k] bf16, pitch ldx.
  *   packed    one layer (experts 1) from dycl_op_linear_pack.
  *   bias, gate_bias  [n] float32 or NULL (gate_bias only if gated).
- *   act       0 none, 1 ReLU, 2 exact GELU, 3 SiLU.
+ *   act       0 none, 1 ReLU, 2 exact GELU, 3 SiLU; of NaN each is NaN.
  *   residual  [m][n] bf16, pitch ldr, or NULL.
  *   y         [m][n] y_type, pitch ldy; may be the residual itself if bf16.
  *   workspace dycl_op_linear_workspace(x, ldx, m, k, n, gated) bytes, 16-byte aligned:

@@ -54,7 +54,7 @@ __device__ __forceinline__ int scan_lanes(int v) {
 __device__ __forceinline__ float sigmoid_fast(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 
 __device__ __forceinline__ float token_act(float v, int act) {
-  if (act == TACT_RELU) return v > 0.f ? v : 0.f;
+  if (act == TACT_RELU) return v < 0.f ? 0.f : v;   // (NaN stays NaN)
   if (act == TACT_GELU) return gelu_f32(v);
   if (act == TACT_SILU) return v * sigmoid_fast(v);
   return v;
