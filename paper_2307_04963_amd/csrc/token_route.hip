@@ -175,7 +175,8 @@ __device__ __forceinline__ void choose(const RouteArgs& p, const Layout& l, cons
     if (l.lanes > 4) merge2(a, b, dpp<0x141>(a), dpp<0x141>(b));        // the other four of eight
     if (l.lanes > 8) merge2(a, b, dpp<0x140>(a), dpp<0x140>(b));        // the other eight of 16
     if (l.lanes > 16) merge2(a, b, __shfl_xor(a, 16), __shfl_xor(b, 16));
-    const float score = b == kClosed ? a : a + b;
+    // half the sum: that of two lowest values is finite, above a group with none open
+    const float score = b == kClosed ? 0.5f * a : 0.5f * a + 0.5f * b;
     int better = 0;
     for (int g = 0; g < p.groups; ++g) {
       const float o = lane_value(score, g * l.lanes);
