@@ -85,7 +85,10 @@ def partition(flags: torch.Tensor, rows: torch.Tensor):
 
 
 def gather(t: torch.Tensor, positions: torch.Tensor) -> torch.Tensor:
-    """dycl_op_move_rows: the rows of t at `positions` (row bytes a multiple of 16)."""
+    """dycl_op_move_rows: the rows of t at `positions` (row bytes a multiple of 16).  It takes packed, 16-byte aligned rows;
+    others, which the operators read where they are, are packed first."""
+    if not t.is_contiguous() or t.data_ptr() % 16:
+        t = t.clone(memory_format=torch.contiguous_format)
     out = torch.empty((len(positions), t.shape[1]), dtype=t.dtype, device=t.device)
     _lib.check(_lib.lib.dycl_op_move_rows(out.data_ptr(), None, t.data_ptr(), positions.data_ptr(), t.shape[1] * t.element_size(),
                                           len(positions), torch.cuda.current_stream(t.device).cuda_stream))
