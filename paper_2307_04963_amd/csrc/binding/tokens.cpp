@@ -12,6 +12,7 @@
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -63,7 +64,10 @@ struct Args {
     PyObject* o = next();
     if (optional && o == Py_None) return nullptr;
     if (!THPVariable_Check(o)) refuse(std::string(what) + " must be a tensor" + (optional ? " or None" : ""));
-    return &THPVariable_Unpack(o);
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+      refuse(std::string(what) + " requires grad, and the token operators have no backward: call them under torch.no_grad(), or detach it");
+    return &t;
   }
   long integer() {
     const long v = PyLong_AsLong(next());
