@@ -41,8 +41,11 @@ def _of(table: dict, key, what: str) -> int:
 
 
 def _call(stream, f, *args):
+    """f on the given stream; args[0] is the tensor that says where the call runs."""
     if stream is None:
         return f(*args)
+    if isinstance(args[0], torch.Tensor) and stream.device != args[0].device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {args[0].device}")
     with torch.cuda.stream(stream):
         return f(*args)
 
