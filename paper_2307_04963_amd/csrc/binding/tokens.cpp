@@ -209,6 +209,9 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t count) {
     const float *pw = floats(post_w, "post_weight", {d}, dev), *pb = floats(post_b, "post_bias", {d}, dev);
     const float *qw = floats(pre_w, "pre_weight", {d}, dev), *qb = floats(pre_b, "pre_bias", {d}, dev);
     if (u_in && pre == DYCL_NORM_NONE) refuse("u needs a pre norm");
+    // (as the C interface, which a call that leaves x as it is does not come to)
+    if (!y && (post != DYCL_NORM_NONE || rg || cs || pw || pb)) refuse("a post norm or a gate needs y");
+    if (pre == DYCL_NORM_NONE && (qw || qb)) refuse("pre weights need a pre norm");
     if (d > INT32_MAX) refuse("d out of range");
     const c10::DeviceGuard on(dev);
     at::Tensor h, u;

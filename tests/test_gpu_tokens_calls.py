@@ -36,3 +36,18 @@ def test_tensors_that_require_grad(ex):
         with torch.inference_mode():
             call(lambda t: t)
         call(lambda t: want(t).detach())
+
+
+def test_a_norm_of_nothing(ex):
+    """Without y, a pre norm or a scale x is the result as it is; weights and norms given all the same are a mistake."""
+    from paper_2307_04963_amd._lib import DyclError
+    x, w, r = torch.ones((4, 64), dtype=B, device="cuda"), torch.ones(64, device="cuda"), torch.ones(4, device="cuda")
+    assert ex.norm(x)[0] is x
+    for more in ({}, {"pre": "rms"}):
+        for bad in ({"post": "rms"}, {"post_weight": w}, {"post_bias": w}, {"channel_scale": w}, {"row_gate": r}, {"gate": x}):
+            with pytest.raises((ValueError, DyclError)):
+                ex.norm(x, **bad, **more)
+                print("accepted:", bad, more)
+    for bad in ({"pre_weight": w}, {"pre_bias": w}):
+        with pytest.raises((ValueError, DyclError)):
+            ex.norm(x, **bad)
