@@ -5,7 +5,9 @@ _tokens.so, the Python binding of its token operators.
 ``csrc/`` with hipcc for gfx950 and links ``libdycl.so`` next to this file, then
 ``csrc/binding/`` with the host compiler against torch's headers.
 It always recompiles (objects go to ``_build/`` at the repository root).
-No GPU is needed: hipcc cross-compiles.
+No GPU is needed: hipcc cross-compiles.  The library itself needs hipcc alone:
+where torch, its or Python's headers or the host compiler are missing, the
+binding is left out (importing ``experts`` says so) and the rest is built.
 """
 
 from __future__ import annotations
@@ -16,6 +18,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -46,16 +49,33 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _cxx() -> str:
+    return os.environ.get("CXX", "g++")
+
+
+def _binding_lacks() -> str:
+    """What the binding cannot be built without and is not here, or ""."""
+    if not shutil.which(_cxx()):
+        return f"the host compiler {_cxx()}"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    try:
+        from torch.utils import cpp_extension
+    except ImportError:
+        return "torch"
+    if not any(os.path.exists(os.path.join(d, "ATen", "ATen.h")) for d in cpp_extension.include_paths()):
+        return "torch's C++ headers"
+    return ""
+
+
 def _compile_binding() -> str:
     """The binding's object: host code that sees torch's and HIP's headers."""
-    import sysconfig
-
     import torch
     from torch.utils import cpp_extension
     src = os.path.join(CSRC, "binding", "tokens.cpp")
     obj = os.path.join(BUILD, "binding_tokens.o")
     rocm = os.path.dirname(os.path.dirname(hipcc()))
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+    cmd = [_cxx(), "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", sysconfig.get_paths()["include"],
            "-isystem", os.path.join(rocm, "include")]
     for inc in cpp_extension.include_paths():
@@ -72,7 +92,7 @@ def _link_binding(obj: str) -> None:
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = BINDING + ".tmp"
     # (torch's libraries are in the process already; the library beside it is found by its own folder)
-    cmd = [os.environ.get("CXX", "g++"), "-shared", "-fPIC", "-o", tmp, obj, "-L" + PKG, "-l:libdycl.so", "-L" + libs, "-lc10", "-lc10_hip",
+    cmd = [_cxx(), "-shared", "-fPIC", "-o", tmp, obj, "-L" + PKG, "-l:libdycl.so", "-L" + libs, "-lc10", "-lc10_hip",
            "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
@@ -84,10 +104,10 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.cpp")) + glob.glob(os.path.join(CSRC, "*.hip")))
     workers = min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
+    lacks = _binding_lacks()
     with cf.ThreadPoolExecutor(workers) as ex:
-        binding = ex.submit(_compile_binding)
+        binding = None if lacks else ex.submit(_compile_binding)
         objs = list(ex.map(_compile, srcs))
-        binding_obj = binding.result()
     tmp = OUT + ".tmp"
     cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -101,7 +121,12 @@ def build(verbose: bool = False) -> str:
         os.remove(tmp)
         raise RuntimeError("undefined symbols in the library:\n" + "\n".join(missing[:20]))
     os.replace(tmp, OUT)
-    _link_binding(binding_obj)
+    if binding is None:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)             # (of another library)
+        print(f"built {OUT}; without {lacks} the token operators' Python binding is left out", file=sys.stderr, flush=True)
+        return OUT
+    _link_binding(binding.result())
     if verbose:
         print("built", OUT, "and", BINDING, flush=True)
     return OUT
