@@ -720,35 +720,36 @@ void ring(const ProductArgs& a, hipStream_t s) {
 
 // Which kernel: the one whose estimate is least.  A round of tiles (256 CUs, per_cu
 // workgroups each) takes `round` microseconds and `full` per 64 inputs, `alone` where
-// each CU has one; fitted to 373 plain and 356 gated products of 16 to 8192 rows, 512
-// to 8192 outputs and 256 to 8192 inputs, their weights from memory: the choice is 0.5% and
-// 0.2% slower there than each product's best.  Leaving a shape out costs 0.2 to 4% on
-// average.  Beside each, us of a product of its own and of the next best without it.
+// each CU has one; fitted to 457 plain and 443 gated products of 1 to 8192 rows, 512
+// to 20000 outputs and 256 to 8192 inputs, their weights from memory: the choice is 0.2% and
+// 0.3% slower there than each product's best.  Leaving a shape out costs 0.4 to 3% on
+// average.  Beside some, us of a product of their own and of another shape.
 // (rows x inputs x outputs; gated: two products.)
 struct Shape {
   int bm, bn, per_cu;
   float alone, full, round;
 };
 constexpr Shape kPlain[] = {
-    {256, 256, 1, 1.185f, 1.599f, 9.5f},
-    {128, 256, 2, 0.960f, 1.989f, 5.4f},
-    {64, 128, 2, 0.423f, 0.688f, 3.6f},
-    {64, 128, 1, 0.391f, 0.392f, 3.5f},    // 300 x 4096 x 4096: 29.5 (64 x 128, two per CU: 31.6)
-    {64, 64, 1, 0.263f, 0.260f, 3.3f},     // 256 x 4096 x 4096: 20.8 (32 x 64: 30.5)
-    {32, 64, 1, 0.173f, 0.178f, 3.2f},     // 100 x 4096 x 4096: 15.5 (32 x 32: 19.5)
-    {32, 32, 1, 0.115f, 0.118f, 3.2f},     // 48 x 4096 x 4096: 11.9 (32 x 64: 16.0)
-    {16, 32, 1, 0.082f, 0.084f, 3.3f},     // 1 x 4096 x 4096: 10.1 (three per CU: 16.5)
-    {16, 32, 3, 0.144f, 0.221f, 3.0f},     // 4 x 1024 x 20000: 10.3 (one per CU: 14.4)
+    {256, 256, 1, 1.20f, 1.548f, 10.0f},
+    {128, 256, 2, 1.00f, 2.045f, 5.5f},
+    {64, 128, 2, 0.441f, 0.716f, 3.5f},
+    {64, 128, 1, 0.415f, 0.391f, 3.4f},    // 300 x 4096 x 4096: 29.5 (64 x 128, two per CU: 31.6)
+    {64, 64, 1, 0.266f, 0.259f, 3.2f},     // 256 x 4096 x 4096: 20.8 (32 x 64: 30.5)
+    {32, 64, 1, 0.178f, 0.180f, 3.1f},     // 100 x 4096 x 4096: 15.5 (32 x 32: 19.5)
+    {32, 32, 1, 0.114f, 0.127f, 3.2f},     // 48 x 4096 x 4096: 11.9 (32 x 64: 16.0)
+    {16, 32, 1, 0.079f, 0.099f, 3.3f},     // 1 x 4096 x 4096: 10.1
+    {16, 32, 4, 0.160f, 0.266f, 2.9f},     // 4 x 1024 x 20000: 10.0 (one per CU: 14.4)
 };
 constexpr Shape kGated[] = {
-    {256, 256, 1, 1.185f, 1.566f, 8.7f},
-    {128, 256, 2, 0.989f, 1.932f, 5.0f},
-    {64, 128, 2, 0.429f, 0.680f, 3.8f},
-    {64, 128, 1, 0.408f, 0.421f, 3.6f},    // 512 x 2048 x 2048: 16.8 (two per CU: 17.6)
-    {64, 64, 1, 0.276f, 0.285f, 3.6f},     // 256 x 2048 x 2048: 12.9 (32 x 64: 18.7)
-    {32, 64, 1, 0.192f, 0.196f, 3.5f},     // 64 x 4096 x 4096: 19.4 (64 x 64: 23.8)
-    {16, 64, 1, 0.166f, 0.169f, 3.2f},     // 1 x 4096 x 4096: 16.3 (32 x 64: 16.7)
-    {16, 64, 2, 0.210f, 0.286f, 3.2f},     // 16 rows of 8 of 64 experts, 2048 -> 2 x 1024 -> 2048: 130 a call (one per CU: 138)
+    {256, 256, 1, 1.22f, 1.547f, 8.3f},
+    {128, 256, 2, 1.05f, 1.936f, 4.7f},
+    {64, 128, 2, 0.423f, 0.727f, 3.7f},
+    {64, 128, 1, 0.415f, 0.417f, 3.5f},    // 512 x 2048 x 2048: 16.8 (two per CU: 17.6)
+    {64, 64, 1, 0.273f, 0.290f, 3.6f},     // 256 x 2048 x 2048: 12.9 (32 x 64: 18.7)
+    {32, 64, 1, 0.190f, 0.206f, 3.4f},     // 64 x 4096 x 4096: 19.4 (64 x 64: 23.8)
+    {16, 64, 1, 0.165f, 0.177f, 3.2f},     // 1 x 4096 x 4096: 16.3 (32 x 64: 16.7)
+    {16, 64, 2, 0.215f, 0.300f, 3.1f},     // 16 rows of 8 of 64 experts, 2048 -> 2 x 1024 -> 2048: 130 a call (one per CU: 138)
+    {16, 64, 5, 0.360f, 0.541f, 3.0f},     // 9 rows of 5 of 128 experts, 784 -> 2 x 960 -> 784: 38 a call (two per CU: 45)
 };
 
 // Estimated time of a shape for a layer's rows (with a partition: of the average
@@ -801,7 +802,7 @@ void plain(const ProductArgs& a, int shape, hipStream_t s) {
     case 5: return ring<32, 64, 2, 2, 8, 4, 3, false>(a, s);
     case 6: return ring<32, 32, 2, 2, 8, 4, 4, false>(a, s);
     case 7: return ring<16, 32, 1, 2, 8, 8, 3, false>(a, s);
-    default: return ring<16, 32, 1, 2, 8, 4, 2, false>(a, s);
+    default: return ring<16, 32, 1, 2, 4, 2, 3, false>(a, s);
   }
 }
 
@@ -814,7 +815,8 @@ void gated(const ProductArgs& a, int shape, hipStream_t s) {
     case 4: return ring<64, 64, 4, 1, 8, 2, 3, true>(a, s);
     case 5: return ring<32, 64, 2, 2, 8, 4, 3, true>(a, s);
     case 6: return ring<16, 64, 1, 4, 8, 4, 3, true>(a, s);
-    default: return ring<16, 64, 1, 4, 4, 2, 3, true>(a, s);
+    case 7: return ring<16, 64, 1, 4, 4, 2, 3, true>(a, s);
+    default: return ring<16, 64, 1, 2, 2, 1, 3, true>(a, s);
   }
 }
 

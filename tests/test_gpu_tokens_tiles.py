@@ -11,8 +11,8 @@ import torch
 from paper_2307_04963_amd import _lib
 
 # rows and outputs of a tile, workgroups per CU
-PLAIN = [(256, 256, 1), (128, 256, 2), (64, 128, 2), (64, 128, 1), (64, 64, 1), (32, 64, 1), (32, 32, 1), (16, 32, 3), (16, 32, 1)]
-GATED = [(256, 128, 1), (128, 128, 2), (64, 64, 2), (64, 64, 1), (64, 32, 1), (32, 32, 1), (16, 32, 2), (16, 32, 1)]
+PLAIN = [(256, 256, 1), (128, 256, 2), (64, 128, 2), (64, 128, 1), (64, 64, 1), (32, 64, 1), (32, 32, 1), (16, 32, 4), (16, 32, 1)]
+GATED = [(256, 128, 1), (128, 128, 2), (64, 64, 2), (64, 64, 1), (64, 32, 1), (32, 32, 1), (16, 32, 5), (16, 32, 2), (16, 32, 1)]
 
 # (rows, outputs, inputs): last tiles of 1, 128, 129 and 255 rows, outputs that end inside a strip, inputs inside a step
 LINEAR = {
@@ -20,9 +20,9 @@ LINEAR = {
             (513, 8200, 72), (1300, 3100, 64), (1025, 4104, 520), (8193, 200, 72), (700, 4104, 264), (65, 8200, 72), (300, 4104, 264),
             (33, 8200, 72), (1025, 777, 200), (1, 8200, 264), (100, 3100, 520), (17, 4104, 72), (33, 3100, 520), (1300, 33, 64),
             (5, 4104, 136), (1, 33, 264), (65, 200, 1032)],
-    True: [(513, 8200, 264), (640, 8200, 264), (641, 8200, 264), (767, 8200, 264), (1300, 3100, 264), (200, 8200, 64), (2177, 4104, 136),
+    True: [(513, 8200, 520), (640, 8200, 520), (641, 8200, 520), (767, 8200, 520), (1300, 3100, 520), (200, 8200, 64), (2177, 4104, 136),
            (65, 8200, 72), (2049, 777, 200), (17, 8200, 1032), (2177, 330, 200), (4097, 33, 72), (300, 1500, 200), (17, 4104, 200),
-           (33, 3100, 1032), (200, 1032, 64), (1, 8200, 136), (1, 33, 64), (65, 330, 200)],
+           (33, 3100, 1032), (4097, 33, 136), (100, 4104, 64), (17, 8200, 64), (1, 33, 64), (33, 2056, 64), (65, 330, 200)],
 }
 
 # (pairs of all 8 experts, d, f): the first layer has f outputs on d inputs, the second d on f
@@ -30,7 +30,7 @@ EXPERTS = {
     False: [(8200, 1032, 1032), (2300, 2056, 2056), (700, 264, 264), (513, 777, 72), (2049, 33, 520), (300, 520, 264), (40, 520, 520),
             (130, 200, 136), (17, 3100, 72), (700, 3100, 264), (200, 1032, 520)],
     True: [(8200, 1032, 520), (4200, 2056, 520), (1025, 200, 1032), (700, 264, 264), (2049, 264, 200), (4097, 72, 33), (300, 520, 520),
-           (300, 136, 520), (9, 100, 330), (200, 72, 1032)],
+           (300, 136, 520), (9, 100, 330), (200, 72, 1032), (2177, 520, 200), (300, 64, 330)],
 }
 
 
@@ -104,7 +104,7 @@ def spaced(rows, width, pitch, seed):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("m, n, k, gated", [(1025, 8200, 520, False), (513, 8200, 264, True), (513, 8200, 72, False), (300, 4104, 264, False),
+@pytest.mark.parametrize("m, n, k, gated", [(1025, 8200, 520, False), (513, 8200, 520, True), (513, 8200, 72, False), (300, 4104, 264, False),
                                             (100, 3100, 520, False), (65, 330, 200, True)])
 def test_linear_rows_beyond_32_bits(ex, m, n, k, gated):
     """256 rows at this pitch are 2^32 bytes: offsets of 64 bits in a tile."""
