@@ -4,15 +4,18 @@
 // Bound by HBM: x, y and the gate are read once, h and u written once.  T
 // lanes hold a row in registers, so both norms' statistics (float32; the
 // layer norm's variance from the centred values) come from one read.  A
-// workgroup walks over rows with the weights in registers (read for every
-// row they would double the loads), and requests the next row before it
-// reduces the present one.  Rows at any alignment are read 16 bytes per lane; element
-// by element, 1999 rows of 1003 took twice as long.
+// workgroup walks over rows with the weights in registers up to 8192 values (read
+// for every row they would double the loads), and requests the next row before
+// it reduces the present one.  Rows at any alignment are read 16 bytes per lane;
+// element by element, 1999 rows of 1003 took twice as long.  Beyond 16384 values
+// the row ahead does not fit the registers and goes through scratch, from 8193 on
+// where 8 does not divide the row: about half the rate.
 //
 // Measured: 16384 x 4096 in bf16, both norms, 537 MB in 102 us = 5.3 TB/s, about the
 // rate of a plain copy (5.2 to 5.5); 1999 x 1003, x in float32, with a gate, row gates
-// and biases 12 us, where the bytes would take 5 (the weights' first loads and the
-// latencies of a row's chain); 1 x 2048 4 us, a launch.
+// and biases 10 to 12 us, where the bytes would take 5 (three dependent trips to memory
+// before a row ends: the weights, a row's gate and then its values, and the gate's
+// behind the first norm); 1 x 2048 2.8 us, a launch.
 #include "token_dev.hpp"
 
 namespace dycl {
@@ -298,6 +301,11 @@ void by_type(const NormArgs& a, hipStream_t s) {
     a.y_f32 ? launch<T, NV, TAIL, false, true>(a, s) : launch<T, NV, TAIL, false, false>(a, s);
 }
 
+// Lanes per row and pieces of 8 values per lane, both norms over 2^26 values in bf16
+// (us, beside another form that holds the row): 512 as <64, 1> 100 (<64, 2> 122); 1024 as
+// <64, 2> 103 (<256, 1> 119); 2048 as <256, 1> 101 (<64, 4> 100, but 32 rows 3.3 against 5.0);
+// 4096 as <256, 2> 102 (<512, 1> 115); 8192 as <256, 4> 99 (<512, 2> 102); 12288 as <1024, 2> 111
+// (<512, 4> 123); 16384 as <1024, 2> 108 (<512, 4> 120); 16001 180 (189); 32768 171, 20001 314.
 template <bool TAIL>
 void by_size(const NormArgs& a, hipStream_t s) {
   if (a.d <= 512) return by_type<64, 1, TAIL>(a, s);
@@ -305,7 +313,7 @@ void by_size(const NormArgs& a, hipStream_t s) {
   if (a.d <= 2048) return by_type<256, 1, TAIL>(a, s);
   if (a.d <= 4096) return by_type<256, 2, TAIL>(a, s);
   if (a.d <= 8192) return by_type<256, 4, TAIL>(a, s);
-  if (a.d <= 16384) return by_type<512, 4, TAIL>(a, s);
+  if (a.d <= 16384) return by_type<1024, 2, TAIL>(a, s);
   by_type<1024, 4, TAIL>(a, s);
 }
 
