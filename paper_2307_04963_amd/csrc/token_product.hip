@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void token_pack_kernel(const uint16_t* w, cons
 }
 
 // Rows that no 16-byte load could start at, or whose end a K step would pass, copied to
-// rows of a whole number of steps: 1237 x 1003 in 3 to 4 us, mostly the launch.
+// rows of a whole number of steps: 1237 x 1003 in 3.7 to 4.4 us, mostly the launch.
 __global__ __launch_bounds__(256) void token_align_kernel(const uint16_t* x, int64_t ldx, int64_t n, int d, uint16_t* out,
                                                           int64_t ldo) {
   const int64_t per = ldo / 8;
@@ -271,9 +271,9 @@ template <int TB, int RB, bool GATED>
 __device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& tile, int row0, int strip, const f32x4 (&acc)[TB][RB]) {
   constexpr int NB = GATED ? 4 : 2;
   const int lane = threadIdx.x & 63;
-  // strip after strip of a row, so that a wave's two pieces of a line leave together:
-  // 8192 rows of 8 of 64 experts 919 us in 256 x 256 tiles and 277 MB written by the second
-  // product; row after row of a strip 940 and 348
+  // strip after strip of a row, so that a wave's two pieces of a line leave together
+  // (8192 rows of 8 of 64 experts, when their results were 16 bits wide: 919 us in 256 x
+  // 256 tiles and 277 MB written by the second product; row after row of a strip 940 and 348)
   auto finish = [&](auto act) __attribute__((always_inline)) {
     constexpr int C = RB / NB;
     const int o0 = strip * kStrip + 8 * (lane >> 4);
@@ -320,8 +320,7 @@ __device__ __forceinline__ void tile_epilogue(const ProductArgs& p, const Tile& 
 // of step h + 1), and what a wave requested for step h + 1 has to be there before
 // half 2 h + 2: it waits for that at the end of its read of step h.  With the waves
 // in step, all reading and then all multiplying, 8192 x 4096 x 8192 took 4 % longer;
-// with four waves of 128 x 128 each, 14 %; with 32 x 32 x 16 instructions 9 %.  The
-// matrix cores are 68 % busy at the clock that this load leaves.
+// with four waves of 128 x 128 each, 14 %; with 32 x 32 x 16 instructions 9 %.
 __device__ __align__(16) const uint16_t g_zeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 
 template <int N>
@@ -450,12 +449,11 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const Tile& t
 // rows or fewer, takes half the time.  128 x 256 tiles on three stages leave room for two
 // workgroups, one's epilogue beside the other's products: better for short K.
 //
-// Measured: gated 8192 x 4096 x 4096 398 us = 1.38 PF, matrix cores 73% busy at the
+// Measured: gated 8192 x 4096 x 4096 395 us = 1.39 PF, matrix cores 72% busy at the
 // clock that the power limit leaves (1.8 to 1.95 GHz); a library's product of that size
-// reaches 1.5 PF.  8192 rows of 8 of 64 experts: 2048 -> 2 x 1024 in 560 us (0.98 PF; 2.2
-// GB pass the L2s for 0.8 GB of rows and weights), 1024 -> 2048 in 337 us (0.82 PF).  Slower:
-// matrix instructions of 32 x 32 results (9%), four waves of 128 x 128 (14%), all waves
-// in step (4%).
+// reaches 1.5 PF.  8192 rows of 8 of 64 experts: 2048 -> 2 x 1024 in 549 us (1.0 PF; 2.3
+// GB pass the L2s for 0.8 GB of rows and weights), 1024 -> 2048 in 402 us (0.68 PF; 0.94 GB
+// read, 0.54 GB of float32 results written).
 template <int BM, bool GATED>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(BM == 256 ? 2 : 4)))
 void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
@@ -478,6 +476,13 @@ void token_tile_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
 // waves multiply, each its part of the tile over all steps in order, the order of the
 // large tiles: a row's sums are the same bits whichever kernel takes it.  One barrier
 // per stage: behind it, the stage read a turn ago takes the loads of the stage S - 1 ahead.
+// Where RB is less than a strip's blocks, its sums meet in LDS.
+//
+// Few rows are bound by the weights' way from memory: 5 x 4096 x 4096, 34 MB in 7.3 us; one
+// row through eight experts 2048 -> 2 x 1024 -> 2048, 101 MB in 11.8 + 7.9 us = 5.1 TB/s; 333
+// rows crowded on about half of 32 experts, 1024 -> 2048 -> 1024, 155 MB in 17.6 + 17.4 us =
+// 4.4 TB/s.  More rows are bound by the stages' turns (one barrier and a first read of LDS
+// each) while a CU holds one or two tiles: 1237 x 1008 x 777 10.9 us on 140 CUs.
 template <int BM, int BN, int WM, int WN, int W, int KT, int S, bool GATED>
 __global__ __launch_bounds__(64 * W) void token_ring_kernel(ProductArgs p, int strips, int steps, int col_tiles) {
   constexpr int NB = GATED ? 4 : 2;                 // blocks per strip and step
@@ -629,7 +634,8 @@ __global__ __launch_bounds__(64 * W) void token_ring_kernel(ProductArgs p, int s
 // Eight outputs per lane, float32 until the one rounding of the sum: held in fewer bits,
 // the results' own roundings come to more than the sum's.  A row's slots and weights
 // come first, then up to eight experts' results are requested together: taken one by
-// one, each waited for its slot and then for its values.
+// one, each waited for its slot and then for its values.  Bound by HBM: 8192 rows of 2048,
+// 8 experts each, 606 MB in 124 us = 4.9 TB/s.
 __global__ __launch_bounds__(256) void token_combine_kernel(CombineArgs p) {
   const int per = (p.d + 7) / 8;
   const int64_t all = p.n * per;
@@ -754,11 +760,11 @@ constexpr Shape kGated[] = {
 
 // Estimated time of a shape for a layer's rows (with a partition: of the average
 // expert, whose last tile is half full; of 256 rows, one up to half full takes half
-// the time).  For the two products of 18 expert layers (1 to 8192 rows, 8 to 128 experts,
-// 1 to 8 of them a row, skewed or not) the choice is 0.9% slower than each product's best on
-// the average, at worst 9% (2048 rows of 8 of 128 experts: 128 rows each, where 256 x 256
+// the time).  For the two products of 20 expert layers (1 to 8192 rows, 8 to 128 experts,
+// 1 to 8 of them a row, skewed or not) the choice is 0.8% slower than each product's best on
+// the average, at worst 10% (2048 rows of 8 of 128 experts: 128 rows each, where 256 x 256
 // tiles beat 128 x 256).  Steps taken as 7 or 14% longer for experts' weights, as one size
-// of them would have it, make that 1.2%.
+// of them would have it, make that 1.0%.
 inline float estimate(const Shape& t, const ProductArgs& a, bool gated) {
   const float steps = static_cast<float>(steps_of(a.K) / 2);
   const float cols = ceilf(strips_of(a.N) * (gated ? 64.f : 32.f) / t.bn);

@@ -9,9 +9,10 @@
 // and that lane's next best.  Bound by instruction issue: 467 vector instructions for
 // a row of 256 experts in 8 groups, eight of them chosen, the rounds half of that.
 //
-// Measured: 65536 rows of 256 experts, 8 chosen in 4 of 8 groups: choice 59 us, sums
+// Measured: 65536 rows of 256 experts, 8 chosen in 4 of 8 groups: choice 60 us, sums
 // 5, places 9 (the bytes would take 14); 32768 rows of 64, 14 + 4 + 4 us; 24 rows of
-// 256, one launch, 9 us: the latency of one wave's rounds.
+// 256, one launch, 8.5 us: up to 64 rows are one workgroup of 16 waves, so eight of them
+// take two rows one after the other, 16 rounds of dependent steps at 0.4 us.
 //
 // The partition works on blocks of 64 rows: an expert's rows in a block are one
 // 64-bit mask in LDS, so a pair's rank among the block's is a bit count and
