@@ -131,9 +131,9 @@ int dycl_op_linear_pack(const uint16_t* w, const uint16_t* gate, int experts, in
  *   workspace dycl_op_linear_workspace(x, ldx, m, k, n, gated) bytes, 16-byte aligned:
  *             0 (NULL) where x is 16-byte aligned and k and ldx are
  *             multiples of 8, room for aligned rows otherwise.
- * m >= 0 (0 does nothing).  A launch holds 2^23 - 1 tiles; more than that of
- * the largest (256 rows x 256 outputs, 128 gated) return DYCL_E_INVALID, here
- * and below.
+ * m >= 0 (0 does nothing).  A launch holds fewer than 2^23 - 1 tiles: as many
+ * or more of the largest (256 rows x 256 outputs, 128 gated) return
+ * DYCL_E_INVALID, here and below.
  *
  * dycl_op_linear_tile tells which kernel a product takes: tile receives the
  * rows and outputs of its tiles and how many of them a CU takes together.
