@@ -27,6 +27,10 @@ OPS_EXPORTS = ["dycl_op_compact_workspace", "dycl_op_compact", "dycl_op_compact_
 TOKENS_EXPORTS = ["dycl_op_norm", "dycl_op_route_workspace", "dycl_op_route", "dycl_op_linear_packed_bytes", "dycl_op_linear_pack",
                   "dycl_op_linear_tile", "dycl_op_linear_workspace", "dycl_op_linear", "dycl_op_experts_workspace", "dycl_op_experts"]
 
+# every symbol include/dycl_decode.h declares
+DECODE_EXPORTS = ["dycl_op_rotate", "dycl_op_append", "dycl_op_attend_workspace", "dycl_op_attend", "dycl_op_beam_workspace", "dycl_op_beam",
+                  "dycl_op_fork"]
+
 
 class DyclError(RuntimeError):
     def __init__(self, code: int, msg: str):
@@ -120,6 +124,22 @@ def _load():
     lib.dycl_op_experts.argtypes = [vp, i64, i64, i32, i32, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp,
                                     i64, vp, sz, vp]
     lib.dycl_op_experts.restype = i32
+    lib.dycl_op_rotate.argtypes = [vp, i32, i64, vp, vp, i32, i32, f32, i32, i64, i32, i32, vp, i64, vp]
+    lib.dycl_op_rotate.restype = i32
+    lib.dycl_op_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, vp, i32, i32, f32, i64, i32, i32, i32, vp, i64, i64,
+                                   i32, vp, vp, i64, i32, vp]
+    lib.dycl_op_append.restype = i32
+    lib.dycl_op_attend_workspace.argtypes = [i64, i32, i32, i32, i64, i64]
+    lib.dycl_op_attend_workspace.restype = sz
+    lib.dycl_op_attend.argtypes = [vp, i64, i64, i32, i32, i32, f32, vp, vp, i64, i32, vp, i64, i64, i32, vp, vp, i64, i64, vp, i64, vp,
+                                   i64, vp, sz, vp]
+    lib.dycl_op_attend.restype = i32
+    lib.dycl_op_beam_workspace.argtypes = [i64, i32, i32, i32]
+    lib.dycl_op_beam_workspace.restype = sz
+    lib.dycl_op_beam.argtypes = [vp, i32, i64, vp, vp, i32, i64, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.dycl_op_beam.restype = i32
+    lib.dycl_op_fork.argtypes = [vp, i64, vp, i64, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32, vp]
+    lib.dycl_op_fork.restype = i32
     return lib
 
 

@@ -1,5 +1,5 @@
 """Build libdycl.so (the C-ABI library with its gfx950 kernels) in-tree, and
-_tokens.so, the Python binding of its token operators.
+_tokens.so, the Python binding of its token and decoding operators.
 
 ``python -m paper_2307_04963_amd.build`` compiles every source under
 ``csrc/`` with hipcc for gfx950 and links ``libdycl.so`` next to this file, then
@@ -7,7 +7,7 @@ _tokens.so, the Python binding of its token operators.
 It always recompiles (objects go to ``_build/`` at the repository root).
 No GPU is needed: hipcc cross-compiles.  The library itself needs hipcc alone:
 where torch, its or Python's headers or the host compiler are missing, the
-binding is left out (importing ``experts`` says so) and the rest is built.
+binding is left out (importing ``experts`` or ``decoding`` says so) and the rest is built.
 """
 
 from __future__ import annotations
@@ -68,12 +68,11 @@ def _binding_lacks() -> str:
     return ""
 
 
-def _compile_binding() -> str:
-    """The binding's object: host code that sees torch's and HIP's headers."""
+def _compile_binding(src: str) -> str:
+    """An object of the binding: host code that sees torch's and HIP's headers."""
     import torch
     from torch.utils import cpp_extension
-    src = os.path.join(CSRC, "binding", "tokens.cpp")
-    obj = os.path.join(BUILD, "binding_tokens.o")
+    obj = os.path.join(BUILD, "binding_" + os.path.basename(src) + ".o")
     rocm = os.path.dirname(os.path.dirname(hipcc()))
     cmd = [_cxx(), "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", sysconfig.get_paths()["include"],
@@ -87,12 +86,12 @@ def _compile_binding() -> str:
     return obj
 
 
-def _link_binding(obj: str) -> None:
+def _link_binding(objs: list) -> None:
     import torch
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = BINDING + ".tmp"
     # (torch's libraries are in the process already; the library beside it is found by its own folder)
-    cmd = [_cxx(), "-shared", "-fPIC", "-o", tmp, obj, "-L" + PKG, "-l:libdycl.so", "-L" + libs, "-lc10", "-lc10_hip",
+    cmd = [_cxx(), "-shared", "-fPIC", "-o", tmp] + objs + ["-L" + PKG, "-l:libdycl.so", "-L" + libs, "-lc10", "-lc10_hip",
            "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
@@ -106,7 +105,7 @@ def build(verbose: bool = False) -> str:
     workers = min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
     lacks = _binding_lacks()
     with cf.ThreadPoolExecutor(workers) as ex:
-        binding = None if lacks else ex.submit(_compile_binding)
+        binding = None if lacks else [ex.submit(_compile_binding, s) for s in sorted(glob.glob(os.path.join(CSRC, "binding", "*.cpp")))]
         objs = list(ex.map(_compile, srcs))
     tmp = OUT + ".tmp"
     cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
@@ -126,7 +125,7 @@ def build(verbose: bool = False) -> str:
             os.remove(BINDING)             # (of another library)
         print(f"built {OUT}; without {lacks} the token operators' Python binding is left out", file=sys.stderr, flush=True)
         return OUT
-    _link_binding(binding.result())
+    _link_binding([b.result() for b in binding])
     if verbose:
         print("built", OUT, "and", BINDING, flush=True)
     return OUT

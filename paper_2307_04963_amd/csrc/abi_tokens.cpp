@@ -2,31 +2,14 @@
 // checks, workspace layout and launches.  Nothing thrown crosses them.
 #include "../../include/dycl_tokens.h"
 
-#include <string>
-
-#include "abi.hpp"
+#include "abi_checks.hpp"
 #include "tokens.hpp"
 
 namespace {
 
-using dycl::fail;
 using dycl::guarded;
+using namespace dycl::checks;
 using namespace dycl::k;
-
-struct Bad : std::runtime_error {
-  using std::runtime_error::runtime_error;
-};
-
-// throws (mapped to DYCL_E_INVALID) unless ok
-void need(bool ok, const char* op, const char* what) {
-  if (!ok) throw Bad(std::string(op) + ": " + what);
-}
-
-bool at(const void* p, size_t align) { return reinterpret_cast<uintptr_t>(p) % align == 0; }
-
-bool type_ok(int t) { return t == DYCL_BF16 || t == DYCL_F32; }
-
-size_t size_of(int t) { return t == DYCL_F32 ? 4 : 2; }
 
 size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -40,11 +23,7 @@ bool layers_ok(int experts, int n, int k) {
   return experts >= 1 && experts <= kMaxLayers && n >= 1 && n <= kMaxWidth && k >= 1 && k <= kMaxWidth;
 }
 
-constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxPitch = int64_t(1) << 40;
-
 const char* const kTooMany = "more tiles of results than a launch holds";
-
-bool pitch_ok(int64_t ld, int64_t width) { return ld >= width && ld < kMaxPitch; }
 
 }  // namespace
 
