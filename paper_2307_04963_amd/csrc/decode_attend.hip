@@ -15,10 +15,12 @@
 // neighbouring values of its octet's eight rows, whole rows per 16 lanes, and turns that square around
 // in registers for the left operand.  Nothing passes LDS until the end.
 //
-// A workgroup of four waves takes a part, `tiles` tiles per wave; waves join
-// through LDS, parts through the workspace and a second kernel, each in order.
-// The size of a part follows from the capacity, not from the number of rows: a row's bits
-// do not depend on its company.
+// The four waves of a workgroup take a tile each (or two): a part, whose four results are joined through LDS.
+// The parts of 512 keys in order are a run, four runs in order a stretch, and the stretches are joined in order:
+// always the same steps.  How much of that a workgroup does by itself follows from the number of
+// workgroups that there would be: a stretch, requests running ahead of the products; a run; or
+// one part, the quickest.  A second kernel does the rest.  So a row's bits do not depend on the number of
+// rows.
 #include "decode_dev.hpp"
 
 namespace dycl {
@@ -29,14 +31,22 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kTile = 32, kColumns = 16;
 constexpr float kNone = -__builtin_inff(), kLog2e = 1.44269504088896340736f;
 
+// Heads of up to 64 dims take two tiles at once: what is done per tile and part is half the work there.
+template <int DP>
+struct Shape {
+  static constexpr int kTiles = DP <= 64 ? 2 : 1;                  // per wave of a part
+  static constexpr int kPart = kWaves * kTiles * kTile;            // keys of a part
+  static constexpr int kRun = 512 / kPart, kStretch = 2048 / kPart;   // parts of each
+};
+constexpr int kRunKeys = 512, kStretchKeys = 2048, kFour = 4;
+
 // How the keys are divided; the same for all rows.
 struct Parts {
-  int tiles;                     // per wave
-  int keys;                      // of a part
-  uint32_t parts;                // of the longest row
-  uint32_t blocks;                  // of kColumns query heads that share a head
-  float* sums;                   // [row][query head][part][dim], null where one part is all
-  float2* state;                 // [row][query head][part]: maximum (of scores in base 2), sum
+  int keys;                      // that a workgroup takes (a piece): a part, a run or a stretch
+  uint32_t pieces;               // of the longest row (and head)
+  uint32_t blocks;               // of kColumns query heads that share a head
+  float* sums;                   // [row][query head][piece][dim], null where one piece is all
+  float2* state;                 // [row][query head][piece]: maximum (of scores in base 2), sum
 };
 
 // the keys that a row sees: [lo, hi), and the first key of its first part
@@ -52,315 +62,507 @@ __device__ __forceinline__ Span span_of(const AttendArgs& p, int64_t row) {
   return s;
 }
 
+// which of the eight keys from `key` on a row sees
+__device__ __forceinline__ uint32_t octet_of(const Span& s, int64_t key) {
+  const int hi = static_cast<int>(max(int64_t(0), min(int64_t(8), s.hi - key)));
+  const int lo = static_cast<int>(max(int64_t(0), min(int64_t(8), s.lo - key)));
+  return ((1u << hi) - 1) & ~((1u << lo) - 1);
+}
+
+// which of the eight places from `key` on of a mask row of `width` are open
+__device__ __forceinline__ uint32_t open_of(const uint8_t* mask, int64_t key, int64_t width) {
+  typedef uint32_t words __attribute__((ext_vector_type(2), aligned(1)));
+  uint32_t open = 0;
+  if (key + 8 <= width) {
+    const words w = *reinterpret_cast<const words*>(mask + key);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) open |= (w[j / 4] >> 8 * (j % 4) & 0xff ? 1u : 0u) << j;
+  } else {
+    for (int j = 0; key + j < width; ++j) open |= (mask[key + j] ? 1u : 0u) << j;
+  }
+  return open;
+}
+
+// Four values' weighted sums over some keys: of exp2(score - top) * value, and of the weights alone.
+struct Sum {
+  float4 v;
+  float top, total;
+};
+
+// a and b joined; the same operations wherever it is called
+__device__ __forceinline__ Sum join(const Sum& a, const Sum& b) {
+  Sum r;
+  r.top = fmaxf(a.top, b.top);
+  const float base = r.top == kNone ? 0.f : r.top;
+  const float f = __builtin_amdgcn_exp2f(a.top - base), e = __builtin_amdgcn_exp2f(b.top - base);
+  r.v.x = __builtin_fmaf(a.v.x, f, e * b.v.x);
+  r.v.y = __builtin_fmaf(a.v.y, f, e * b.v.y);
+  r.v.z = __builtin_fmaf(a.v.z, f, e * b.v.z);
+  r.v.w = __builtin_fmaf(a.v.w, f, e * b.v.w);
+  r.total = __builtin_fmaf(a.total, f, e * b.total);
+  return r;
+}
+
+__device__ __forceinline__ void finish(uint16_t* out, const Sum& s) {
+  const float inv = s.total == 0.f ? 0.f : 1.f / s.total;
+  out[0] = f2bf(s.v.x * inv), out[1] = f2bf(s.v.y * inv), out[2] = f2bf(s.v.z * inv), out[3] = f2bf(s.v.w * inv);
+}
+
 __device__ __forceinline__ float other_rows_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16));
   return fmaxf(v, __shfl_xor(v, 32));
 }
 
-// Dims of the heads padded to DP; EXACT: they are DP.
-template <int DP, bool EXACT>
-__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs p, Parts d, uint32_t items) {
+// Dims of the heads padded to DP; EXACT: they are DP.  HOLES: there is a mask, and keys that it closes are not read.
+// MANY: a workgroup takes more than one part.
+template <int DP, bool EXACT, bool HOLES, bool MANY>
+__global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_kernel(AttendArgs p, Parts d, uint32_t base) {
+  using S = Shape<DP>;
+  constexpr int U = S::kTiles;
   constexpr int KC = DP / 32;                          // steps of 32 dims of the first product
   constexpr int VW = DP >= 128 ? 8 : 4, VH = DP / (16 * VW);   // a lane's neighbouring values, and how many such
-  constexpr int STRIDE = DP + 4;
-  __shared__ float joint[kWaves][kColumns][STRIDE];
-  __shared__ float2 joint_state[kWaves][kColumns];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr bool QL = MANY && DP >= 128;               // queries in LDS: in registers they are too many
+  extern __shared__ float4 shared[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, g = lane >> 4;
   const PagedArgs& cache = p.cache;
   const int dim = EXACT ? DP : cache.dim;
   const int group = p.q_heads / cache.heads;
   const int64_t page_mask = (int64_t(1) << cache.page_shift) - 1;
-  for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
-    uint32_t rest = item / d.parts;
-    const int64_t part = item - rest * d.parts;
-    const int block = static_cast<int>(rest % d.blocks);
-    rest /= d.blocks;
-    const int head = static_cast<int>(rest % cache.heads);
-    const int64_t row = rest / cache.heads;
-    const Span span = span_of(p, row);
-    const int64_t first = span.begin + part * d.keys;
-    if (d.parts > 1 && first >= span.hi) continue;     // (the same for the whole workgroup)
-    const int columns = min(kColumns, group - block * kColumns);
-    const int q_head = head * group + block * kColumns;
-
-    // queries: the right operand, a column per lane's head
-    bf16x8 q[KC];
+  const uint32_t item = base + blockIdx.x;
+  uint32_t rest = item / d.pieces;
+  const int64_t piece = item - rest * d.pieces;
+  const int block = static_cast<int>(rest % d.blocks);
+  rest /= d.blocks;
+  const int head = static_cast<int>(rest % cache.heads);
+  const int64_t row = rest / cache.heads;
+  const int columns = min(kColumns, group - block * kColumns);
+  const int q_head = head * group + block * kColumns;
+  // LDS: the waves' results, the queries, the sums of the run and of the stretch so far
+  const int live = min(kColumns, group);
+  constexpr int STRIDE = DP + 4;
+  float* joint = reinterpret_cast<float*>(shared);                                     // [wave][column][STRIDE]
+  float2* joint_state = reinterpret_cast<float2*>(joint + kWaves * live * STRIDE);     // [wave][column]
+  uint4* queries = reinterpret_cast<uint4*>(joint_state + kWaves * live);              // [KC][64]
+  float4* so_far = reinterpret_cast<float4*>(queries + (QL ? KC * 64 : 0));            // [run, stretch][column][DP / 4]
+  float2* so_far_state = reinterpret_cast<float2*>(so_far + 2 * live * (DP / 4));
+  // queries: the first product's right operand, a column per lane's head
+  constexpr int QN = QL ? (KC + kWaves - 1) / kWaves : KC;
+  uint4 q[QN];
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      const int at = 32 * c + 8 * g;
-      if (c16 < columns && at < dim) v = load16(p.q + row * p.ldq + static_cast<int64_t>(q_head + c16) * dim + at);
-      q[c] = __builtin_bit_cast(bf16x8, v);
-    }
+  for (int i = 0; i < QN; ++i) {
+    const int c = QL ? i * kWaves + wave : i, at = 32 * c + 8 * g;
+    q[i] = make_uint4(0, 0, 0, 0);
+    if (c < KC && c16 < columns && at < dim) q[i] = load16(p.q + row * p.ldq + static_cast<int64_t>(q_head + c16) * dim + at);
+  }
+  // The pages and the open places of this wave's octets, an octet per lane; requested before the
+  // row's length is known, unless a window hangs on it.
+  const bool in_time = p.window == 0;
+  Span span;
+  if (!in_time) span = span_of(p, row);
+  const int64_t first = (in_time ? 0 : span.begin) + piece * d.keys;
+  const int take = MANY ? d.keys / S::kPart : 1;
+  // the first key of this wave's tiles of part t, and of a lane's octet
+  auto tile_key = [&](int t) { return first + (t * kWaves + wave) * (U * kTile); };
+  const int octet_lane = min(lane, 4 * U * take - 1);
+  const int64_t key_lane = tile_key(octet_lane / (4 * U)) + 8 * (octet_lane % (4 * U));
+  int page_lane = -1;
+  uint32_t here_lane = 0xff;
+  if (cache.sequences > 0) {
+    const int64_t sequence = p.sequence ? p.sequence[row] : row, place = key_lane >> cache.page_shift;
+    const int32_t page = cache.tables[max(int64_t(0), min(sequence, cache.sequences - 1)) * cache.ldt +
+                                      min(place, static_cast<int64_t>(cache.max_pages) - 1)];
+    const bool there = sequence >= 0 && sequence < cache.sequences && place < cache.max_pages;
+    page_lane = there && page >= 0 && page < cache.pages ? page : -1;
+  }
+  if (HOLES) here_lane = open_of(p.mask + row * p.ldm, key_lane, p.max_length);
+  if (in_time) span = span_of(p, row);
+  if (d.pieces > 1 && first >= span.hi) return;       // (the same for the whole workgroup)
+  here_lane &= page_lane < 0 ? 0u : octet_of(span, key_lane);
+  page_lane = max(page_lane, 0);                     // (read, if at all, and not used)
 
-    // this wave's octets' pages, one per lane
-    const int64_t begin = first + static_cast<int64_t>(wave) * d.tiles * kTile;
-    const int64_t sequence = p.sequence ? p.sequence[row] : row;
-    int page_lane = -1;
-    if (lane < 4 * d.tiles && begin + 8 * lane < span.hi) page_lane = static_cast<int>(page_of(cache, sequence, begin + 8 * lane));
-
-    float m = kNone, l = 0.f;
-    f32x4 o[VH * VW];
+  const int parts = MANY ? static_cast<int>(max(int64_t(1), min(static_cast<int64_t>(take), (span.hi - first + S::kPart - 1) / S::kPart))) : 1;
+  // (a tile without keys of its row has none behind it)
+  auto there = [&](int t) { return t < parts && tile_key(t) < span.hi; };
+  uint4 kr[U][2][KC];
+  uint32_t vr[U][8][VH][VW / 2];
+  // A tile's keys and values.  Where there is no further tile, and at closed places, the address is the cache's first: it
+  // stays in the L1, and there are no branches between the loads, around which the compiler would wait for all of them.
+  auto load_keys = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < VH * VW; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    const int tiles = static_cast<int>(max(int64_t(0), min(static_cast<int64_t>(d.tiles), (span.hi - begin + kTile - 1) / kTile)));
-    for (int t = 0; t < tiles; ++t) {
-      const int64_t key = begin + t * kTile;
-      const int page_k = __shfl(page_lane, 4 * t + (c16 >> 2)), page_v = __shfl(page_lane, 4 * t + g);
-      const int64_t key_k = key + 8 * (c16 >> 2) + (c16 & 3), key_v = key + 8 * g;
-      const uint16_t* kp = cache.keys + token_at(cache, max(page_k, 0), head, key_k & page_mask);
-      const uint16_t* vp = cache.values + token_at(cache, max(page_v, 0), head, key_v & page_mask);
-      uint4 kr[2][KC];
+    for (int u = 0; u < U; ++u) {
+      const int octet = 4 * (t * U + u) + (c16 >> 2);
+      const int64_t key = tile_key(t) + u * kTile + 8 * (c16 >> 2) + (c16 & 3);
+      const uint16_t* from = cache.keys + (there(t) ? token_at(cache, __shfl(page_lane, octet), head, key & page_mask) : 0);
+      const uint32_t here = HOLES ? __shfl(here_lane, octet) : 0;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        const uint16_t* row_from = from + 4 * h * dim;
+        if (HOLES) row_from = here >> (4 * h + (c16 & 3)) & 1 ? row_from : cache.keys;
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
-          const int at = 32 * c + 8 * g;
-          kr[h][c] = make_uint4(0, 0, 0, 0);
-          if (EXACT || at < dim) kr[h][c] = *reinterpret_cast<const uint4*>(kp + 4 * h * dim + at);
+          int at = 32 * c + 8 * g;
+          if (!EXACT && at >= dim) at = 0;             // (made 0 before it is used)
+          kr[u][h][c] = *reinterpret_cast<const uint4*>(row_from + at);
         }
-      uint32_t vr[8][VH][VW / 2];
+      }
+    }
+  };
+  auto load_values = [&](int t) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+    for (int u = 0; u < U; ++u) {
+      const int octet = 4 * (t * U + u) + g;
+      const int64_t key = tile_key(t) + u * kTile + 8 * g;
+      const uint16_t* from = cache.values + (there(t) ? token_at(cache, __shfl(page_lane, octet), head, key & page_mask) : 0);
+      const uint32_t here = HOLES ? __shfl(here_lane, octet) : 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint16_t* row_from = from + j * dim;
+        if (HOLES) row_from = here >> j & 1 ? row_from : cache.values;
 #pragma unroll
         for (int h = 0; h < VH; ++h) {
           int at = 16 * VW * h + VW * c16;
           if (!EXACT && at >= dim) at = 0;             // (columns that are not stored)
           if constexpr (VW == 8) {
-            const uint4 v = *reinterpret_cast<const uint4*>(vp + j * dim + at);
-            vr[j][h][0] = v.x, vr[j][h][1] = v.y, vr[j][h][2] = v.z, vr[j][h][3] = v.w;
+            const uint4 v = *reinterpret_cast<const uint4*>(row_from + at);
+            vr[u][j][h][0] = v.x, vr[u][j][h][1] = v.y, vr[u][j][h][2] = v.z, vr[u][j][h][3] = v.w;
           } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(vp + j * dim + at);
-            vr[j][h][0] = v.x, vr[j][h][1] = v.y;
+            const uint2 v = *reinterpret_cast<const uint2*>(row_from + at);
+            vr[u][j][h][0] = v.x, vr[u][j][h][1] = v.y;
           }
         }
+      }
+    }
+  };
 
-      // which keys of the lane's octet count
-      uint32_t here = 0;
-      if (page_v >= 0) {
-        const int hi = static_cast<int>(max(int64_t(0), min(int64_t(8), span.hi - key_v)));
-        const int lo = static_cast<int>(max(int64_t(0), min(int64_t(8), span.lo - key_v)));
-        here = ((1u << hi) - 1) & ~((1u << lo) - 1);
-        if (p.mask) {
-          const uint8_t* mask = p.mask + row * p.ldm + key_v;
-          uint32_t open = 0;
+  if (MANY) {
+    load_keys(0);
+    load_values(0);
+  }
+  if (QL) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (here >> j & 1) open |= (mask[j] != 0 ? 1u : 0u) << j;
-          here = open;
+    for (int i = 0; i < QN; ++i)
+      if (i * kWaves + wave < KC) queries[(i * kWaves + wave) * 64 + lane] = q[i];
+    lds_barrier();                       // (the tile's requests go on)
+  }
+  for (int t = 0; t < parts; ++t) {
+    float m = kNone, l = 0.f;
+    f32x4 o[VH * VW];
+#pragma unroll
+    for (int i = 0; i < VH * VW; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (there(t)) {
+    if (!MANY) {
+      load_keys(t);
+      load_values(t);
+    }
+    float s[U][8];
+    f32x4 score[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) score[u][0] = score[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const bf16x8 q_c = __builtin_bit_cast(bf16x8, QL ? queries[c * 64 + lane] : q[QL ? 0 : c]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4 k = kr[u][h][c];
+          if (!EXACT && 32 * c + 8 * g >= dim) k = make_uint4(0, 0, 0, 0);
+          score[u][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), q_c, score[u][h], 0, 0, 0);
         }
-      }
-
-      float s[8];
+      if (QL) __builtin_amdgcn_sched_barrier(0);       // (else all of the queries are in registers at once)
+    }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int c = 0; c < KC; ++c)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[h][c]), q[c], acc, 0, 0, 0);
+      for (int j = 0; j < 8; ++j) s[u][j] = score[u][j / 4][j % 4] * (p.scale * kLog2e);
+    if (MANY) {
+      load_keys(t + 1);
+      asm volatile("" ::: "memory");     // (the requests stay where they are)
+    }
+    // What turns two keys' values into a pair of the left operand; of a key that does not count a 0 (whatever the cache holds).
+    uint32_t pick[U][2][4];
+    float top = kNone;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[4 * h + r] = acc[r] * (p.scale * kLog2e);
-      }
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) pick[u][0][j] = 0x05040100u, pick[u][1][j] = 0x07060302u;
+      const uint32_t here = __shfl(here_lane, 4 * (t * U + u) + g);
       if (!__all(here == 0xff)) {
+        auto choose = [](uint32_t bits, uint32_t a, uint32_t b) { return (bits & a) | (~bits & b); };
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool on = here >> j & 1;
-          s[j] = on ? s[j] : kNone;
-#pragma unroll
-          for (int h = 0; h < VH; ++h)
-#pragma unroll
-            for (int w = 0; w < VW / 2; ++w) vr[j][h][w] = on ? vr[j][h][w] : 0u;
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t a = static_cast<uint32_t>(static_cast<int32_t>(here << (31 - 2 * j)) >> 31);      // all bits the key's
+          const uint32_t b = static_cast<uint32_t>(static_cast<int32_t>(here << (30 - 2 * j)) >> 31);
+          s[u][2 * j] = __uint_as_float(choose(a, __float_as_uint(s[u][2 * j]), __float_as_uint(kNone)));
+          s[u][2 * j + 1] = __uint_as_float(choose(b, __float_as_uint(s[u][2 * j + 1]), __float_as_uint(kNone)));
+          const uint32_t both = __builtin_amdgcn_perm(b, a, 0x05040100u);
+          pick[u][0][j] = choose(both, 0x05040100u, 0x0c0c0c0cu);
+          pick[u][1][j] = choose(both, 0x07060302u, 0x0c0c0c0cu);
         }
       }
-      float top = s[0];
 #pragma unroll
-      for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
-      const float now = fmaxf(m, other_rows_max(top));
-      const float base = now == kNone ? 0.f : now;
-      const float scale = __builtin_amdgcn_exp2f(m - base);
-      m = now;
-      l *= scale;
-      if (!__all(scale == 1.f)) {
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, s[u][j]);
+    }
+    m = other_rows_max(top);
+    const float all = m == kNone ? 0.f : m;
+    // The weights in two terms (a single bf16 would be off by up to 2^-8 of each): the first is
+    // the weight cut off after 8 bits, the second the rest, never 0, so that a seen key's infinite value
+    // stays one where 0 times it would be NaN; 2^-126 of a value is below its sum's rounding.
+    constexpr float kLeast = 1.17549435e-38f;
+    bf16x8 p_hi[U], p_lo[U];
 #pragma unroll
-        for (int i = 0; i < VH * VW; ++i) o[i] *= scale;
-      }
-      // The weights in two terms (a single bf16 would be off by up to 2^-8 of each): the first is
-      // the weight cut off after 8 bits, the second the rest, never 0, so that a seen key's infinite value
-      // stays one where 0 times it would be NaN; 2^-126 of a value is below its sum's rounding.
-      constexpr float kLeast = 1.17549435e-38f;
+    for (int u = 0; u < U; ++u) {
       uint32_t ph[4], pl[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float a = __builtin_amdgcn_exp2f(s[2 * j] - base), b = __builtin_amdgcn_exp2f(s[2 * j + 1] - base);
+        const float a = __builtin_amdgcn_exp2f(s[u][2 * j] - all), b = __builtin_amdgcn_exp2f(s[u][2 * j + 1] - all);
         l += a;
         l += b;
         ph[j] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
         pl[j] = pack_bf16(fmaxf(a - __uint_as_float(ph[j] << 16), kLeast), fmaxf(b - __uint_as_float(ph[j] & 0xffff0000u), kLeast));
       }
-      const bf16x8 p_hi = __builtin_bit_cast(bf16x8, make_uint4(ph[0], ph[1], ph[2], ph[3]));
-      const bf16x8 p_lo = __builtin_bit_cast(bf16x8, make_uint4(pl[0], pl[1], pl[2], pl[3]));
+      p_hi[u] = __builtin_bit_cast(bf16x8, make_uint4(ph[0], ph[1], ph[2], ph[3]));
+      p_lo[u] = __builtin_bit_cast(bf16x8, make_uint4(pl[0], pl[1], pl[2], pl[3]));
+    }
 #pragma unroll
-      for (int h = 0; h < VH; ++h)
+    for (int h = 0; h < VH; ++h)
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
+      for (int i = 0; i < VW; ++i) {
+        f32x4& acc = o[h * VW + i];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
           uint32_t a[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            a[j] = __builtin_amdgcn_perm(vr[2 * j + 1][h][i / 2], vr[2 * j][h][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+          for (int j = 0; j < 4; ++j) a[j] = __builtin_amdgcn_perm(vr[u][2 * j + 1][h][i / 2], vr[u][2 * j][h][i / 2], pick[u][i & 1][j]);
           const bf16x8 v = __builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3]));
-          f32x4& acc = o[h * VW + i];
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_hi, acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_lo, acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_hi[u], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_lo[u], acc, 0, 0, 0);
         }
+        if (i & 1) __builtin_amdgcn_sched_barrier(0);      // (else all operands are made first, in registers that there are not)
+      }
+    if (MANY) {
+      load_values(t + 1);
+      asm volatile("" ::: "memory");
+    }
     }
 
-    // the waves' results, joined in order
+    // the waves' results joined in order, the part to its run, the run to its stretch
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (c16 < columns) {
-      if (g == 0) joint_state[wave][c16] = make_float2(m, l);
+    if (MANY && t > 0) lds_barrier();    // (the part before has been read)
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));     // (what follows from it is made here, not kept in registers through the loop)
+    const int col_here = thread & 15, g_here = thread >> 4 & 3;
+    if (col_here < columns) {
+      if (g_here == 0) joint_state[wave * live + col_here] = make_float2(m, l);
+      float* to = joint + (wave * live + col_here) * STRIDE + 4 * VW * g_here;
 #pragma unroll
       for (int h = 0; h < VH; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int i = 0; i < VW; i += 4) {
-            const int at = 16 * VW * h + VW * (4 * g + r) + i;
-            *reinterpret_cast<float4*>(&joint[wave][c16][at]) =
+          for (int i = 0; i < VW; i += 4)
+            *reinterpret_cast<float4*>(to + 16 * VW * h + VW * r + i) =
                 make_float4(o[h * VW + i][r], o[h * VW + i + 1][r], o[h * VW + i + 2][r], o[h * VW + i + 3][r]);
-          }
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < columns * (DP / 4); e += kThreads) {
+    lds_barrier();
+    const bool last = t + 1 == parts;
+    const int items = live * (DP / 4);
+    for (int e = thread; e < columns * (DP / 4); e += kThreads) {
       const int col = e / (DP / 4), at = e % (DP / 4) * 4;
-      float top = kNone;
+      Sum sum;
+      sum.top = kNone, sum.total = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, joint_state[w][col].x);
-      const float base = top == kNone ? 0.f : top;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      float total = 0.f;
+      for (int w = 0; w < kWaves; ++w) sum.top = fmaxf(sum.top, joint_state[w * live + col].x);
+      const float all = sum.top == kNone ? 0.f : sum.top;
+      sum.v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(joint_state[w][col].x - base);
-        const float4 v = *reinterpret_cast<const float4*>(&joint[w][col][at]);
-        sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
-        total += f * joint_state[w][col].y;
+        const float2 state = joint_state[w * live + col];
+        const float f = __builtin_amdgcn_exp2f(state.x - all);
+        const float4 v = *reinterpret_cast<const float4*>(joint + (w * live + col) * STRIDE + at);
+        sum.v.x = __builtin_fmaf(f, v.x, sum.v.x), sum.v.y = __builtin_fmaf(f, v.y, sum.v.y);
+        sum.v.z = __builtin_fmaf(f, v.z, sum.v.z), sum.v.w = __builtin_fmaf(f, v.w, sum.v.w);
+        sum.total = __builtin_fmaf(f, state.y, sum.total);
+      }
+      if (MANY) {
+        auto before = [&](int i) { return Sum{so_far[i], so_far_state[i].x, so_far_state[i].y}; };
+        auto keep = [&](int i) { so_far[i] = sum.v, so_far_state[i] = make_float2(sum.top, sum.total); };
+        if (t % S::kRun) sum = join(before(e), sum);
+        if (!last && (t + 1) % S::kRun) {
+          keep(e);
+          continue;
+        }
+        if (t >= S::kRun) sum = join(before(items + e), sum);
+        if (!last) {
+          keep(items + e);
+          continue;
+        }
       }
       if (at >= dim) continue;
       if (d.sums) {
-        const int64_t slot = (row * p.q_heads + q_head + col) * d.parts + part;
-        *reinterpret_cast<float4*>(d.sums + slot * dim + at) = sum;
-        if (at == 0) d.state[slot] = make_float2(top, total);
+        const int64_t slot = (row * p.q_heads + q_head + col) * d.pieces + piece;
+        *reinterpret_cast<float4*>(d.sums + slot * dim + at) = sum.v;
+        if (at == 0) d.state[slot] = make_float2(sum.top, sum.total);
       } else {
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        uint16_t* out = p.out + row * p.ldo + static_cast<int64_t>(q_head + col) * dim + at;
-        out[0] = f2bf(sum.x * inv), out[1] = f2bf(sum.y * inv), out[2] = f2bf(sum.z * inv), out[3] = f2bf(sum.w * inv);
+        finish(p.out + row * p.ldo + static_cast<int64_t>(q_head + col) * dim + at, sum);
       }
     }
-    __syncthreads();             // (the next item's results)
   }
 }
 
-// The parts' sums of one row and query head: threads of DP / 4 columns by slices of parts.
-template <int DP>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, Parts d, int64_t items) {
-  constexpr int COLS = DP / 4, SLICES = kThreads / COLS;
-  __shared__ float tops[kWaves];
-  __shared__ float4 sums[SLICES][COLS];
-  __shared__ float totals[SLICES];
+// The pieces of one row and query head joined, 64 values of the head per workgroup: 16 threads of
+// four values by 16 slices.  A slice joins PER pieces (the parts of a run, the runs of a stretch, or one stretch);
+// then the runs of each stretch (RUNS), then the stretches, in order.
+template <int PER, bool RUNS>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, Parts d, uint32_t base) {
+  constexpr int COLS = 16, SLICES = kThreads / COLS, STEP = SLICES * PER;
+  __shared__ float4 sums[2][SLICES][COLS];
+  __shared__ float2 states[2][SLICES];
   const int col = threadIdx.x % COLS, slice = threadIdx.x / COLS;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t row = item / p.q_heads;
-    const Span span = span_of(p, row);
-    const int64_t parts = span.hi > span.lo ? (span.hi - span.begin + d.keys - 1) / d.keys : 0;
-    const float2* state = d.state + item * d.parts;
-    const float* from = d.sums + item * d.parts * p.cache.dim;
-    float top = kNone;
-    for (int64_t i = threadIdx.x; i < parts; i += kThreads) top = fmaxf(top, state[i].x);
+  const uint32_t chunks = (p.cache.dim + 63) / 64;
+  const uint32_t item = base + blockIdx.x;
+  const uint32_t of = item / chunks;
+  const int at = static_cast<int>(item - of * chunks) * 64 + 4 * col;
+  const int64_t row = of / p.q_heads;
+  const bool live = at < p.cache.dim;
+  const int last = static_cast<int>(d.pieces) - 1;
+  const float2* state = d.state + static_cast<int64_t>(of) * d.pieces;
+  const float* from = d.sums + static_cast<int64_t>(of) * d.pieces * p.cache.dim + (live ? at : 0);
+  float2 s[PER];
+  float4 v[PER];
+  // (requested before the row's length is known, and ahead: past it the workspace holds anything, which is not used)
+  auto request = [&](int i0) {
 #pragma unroll
-    for (int w = 1; w < 64; w *= 2) top = fmaxf(top, __shfl_xor(top, w));
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float base = top == kNone ? 0.f : top;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    float total = 0.f;
-    if (4 * col < p.cache.dim)
-#pragma unroll 4
-      for (int64_t i = slice; i < parts; i += SLICES) {
-        const float2 s = state[i];
-        const float4 v = *reinterpret_cast<const float4*>(from + i * p.cache.dim + 4 * col);
-        const float f = __builtin_amdgcn_exp2f(s.x - base);
-        sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
-        total += f * s.y;
-      }
-    sums[slice][col] = sum;
-    if (col == 0) totals[slice] = total;
-    __syncthreads();
-    if (slice == 0 && 4 * col < p.cache.dim) {
-#pragma unroll
-      for (int i = 1; i < SLICES; ++i) {
-        const float4 v = sums[i][col];
-        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-        total += totals[i];
-      }
-      const float inv = total == 0.f ? 0.f : 1.f / total;
-      uint16_t* out = p.out + row * p.ldo + (item - row * p.q_heads) * p.cache.dim + 4 * col;
-      out[0] = f2bf(sum.x * inv), out[1] = f2bf(sum.y * inv), out[2] = f2bf(sum.z * inv), out[3] = f2bf(sum.w * inv);
+    for (int j = 0; j < PER; ++j) {
+      const int i = min(i0 + slice * PER + j, last);
+      s[j] = state[i];
+      v[j] = *reinterpret_cast<const float4*>(from + static_cast<int64_t>(i) * p.cache.dim);
     }
-    __syncthreads();
+  };
+  request(0);
+  const Span span = span_of(p, row);
+  const int pieces = span.hi > span.lo ? static_cast<int>((span.hi - span.begin + d.keys - 1) / d.keys) : 0;
+  Sum all{make_float4(0.f, 0.f, 0.f, 0.f), kNone, 0.f};
+  for (int i0 = 0, turn = 0; i0 < pieces; i0 += STEP, turn ^= 1) {
+    Sum own{v[0], s[0].x, s[0].y};
+#pragma unroll
+    for (int j = 1; j < PER; ++j)
+      if (i0 + slice * PER + j < pieces) own = join(own, Sum{v[j], s[j].x, s[j].y});
+    const int units = min((pieces - i0 + PER - 1) / PER, SLICES);     // that there are
+    auto put = [&] {
+      sums[turn][slice][col] = own.v;
+      if (col == 0) states[turn][slice] = make_float2(own.top, own.total);
+    };
+    auto get = [&](int i) { return Sum{sums[turn][i][col], states[turn][i].x, states[turn][i].y}; };
+    put();
+    if (i0 + STEP < pieces) request(i0 + STEP);
+    lds_barrier();
+    if constexpr (RUNS) {
+      if (slice % kFour == 0 && slice < units) {
+        for (int i = slice + 1; i < min(slice + kFour, units); ++i) own = join(own, get(i));
+        put();
+      }
+      lds_barrier();
+    }
+    if (slice == 0) {
+      all = i0 == 0 ? own : join(all, own);
+      for (int i = RUNS ? kFour : 1; i < units; i += RUNS ? kFour : 1) all = join(all, get(i));
+    }
   }
+  if (slice == 0 && live) finish(p.out + row * p.ldo + static_cast<int64_t>(of - row * p.q_heads) * p.cache.dim + at, all);
 }
 
-constexpr int64_t kMaxGrid = int64_t(1) << 22;
+// workgroups of a launch (a grid counts fewer than 2^32 threads)
+constexpr uint32_t kMaxGrid = 1u << 23;
 
+int part_keys(int dim) { return dim <= 64 ? Shape<64>::kPart : Shape<128>::kPart; }
+
+// What a workgroup takes, by the stretches that there are (heads of the cache x rows x capacity): a whole one from three per CU on
+// (768 of 128 dims: 146 us, in runs 149, in parts 159; 1024: 188, 195, 210), but from one per CU on if rows are of 16 or
+// more, whose unequal lengths then leave little idle (256 of 256 dims: 95 + 7 us, 106 + 8 in runs); fewer leave CUs idle
+// and each takes 20 to 60 us by itself (64 of 128 dims: 34 us, 17 in runs, 18 in parts).  Runs from one stretch per CU on
+// (384 of 128 dims: 77 us, in parts 83), for 64 dims never (384: 36 and 38, with a mask 33 and 30).
 Parts parts_of(int64_t n, int q_heads, int heads, int dim, int64_t max_length, int64_t window, void* workspace) {
   Parts d;
   const int64_t longest = window ? std::min(max_length, window + kTile - 1) : max_length;
   const int group = q_heads / heads;
-  d.tiles = longest <= 4096 ? 1 : 4;
-  d.keys = kWaves * kTile * d.tiles;
-  d.parts = static_cast<uint32_t>(std::max<int64_t>(1, (longest + d.keys - 1) / d.keys));
   d.blocks = static_cast<uint32_t>((group + kColumns - 1) / kColumns);
-  d.sums = d.parts > 1 ? static_cast<float*>(workspace) : nullptr;
-  d.state = d.sums ? reinterpret_cast<float2*>(d.sums + n * q_heads * d.parts * dim) : nullptr;
+  auto pieces = [&](int keys) { return std::max<int64_t>(1, (longest + keys - 1) / keys); };
+  const int64_t groups = n * heads * d.blocks;
+  const int64_t stretches = groups * longest / kStretchKeys;
+  d.keys = stretches >= (longest >= 16 * kStretchKeys ? 256 : 768) ? kStretchKeys : stretches >= 256 && dim > 64 ? kRunKeys : part_keys(dim);
+  d.pieces = static_cast<uint32_t>(pieces(d.keys));
+  d.sums = d.pieces > 1 ? static_cast<float*>(workspace) : nullptr;
+  d.state = d.sums ? reinterpret_cast<float2*>(d.sums + n * q_heads * d.pieces * dim) : nullptr;
   return d;
+}
+
+template <int DP, bool EXACT, bool HOLES, bool MANY>
+void launch(const AttendArgs& a, const Parts& d, uint32_t items, hipStream_t stream) {
+  const int live = std::min(kColumns, a.q_heads / a.cache.heads);
+  const size_t lds = static_cast<size_t>(kWaves) * live * (4 * (DP + 4) + 8) + (MANY && DP >= 128 ? DP / 32 * 1024 : 0) +
+                     (MANY ? static_cast<size_t>(2 * live) * (DP / 4) * 24 : 0);
+  for (uint32_t base = 0; base < items; base += kMaxGrid) {
+    hipLaunchKernelGGL((attend_kernel<DP, EXACT, HOLES, MANY>), dim3(std::min(items - base, kMaxGrid)), dim3(kThreads), lds, stream, a, d, base);
+    launched("attention");
+  }
+}
+
+template <int DP, bool EXACT, bool HOLES>
+void launch(const AttendArgs& a, const Parts& d, uint32_t items, hipStream_t stream) {
+  if (d.keys > Shape<DP>::kPart)
+    launch<DP, EXACT, HOLES, true>(a, d, items, stream);
+  else
+    launch<DP, EXACT, HOLES, false>(a, d, items, stream);
 }
 
 template <int DP>
 void launch(const AttendArgs& a, const Parts& d, uint32_t items, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, kMaxGrid)));
-  if (a.cache.dim == DP)
-    hipLaunchKernelGGL((attend_kernel<DP, true>), grid, dim3(kThreads), 0, stream, a, d, items);
+  if (a.cache.dim == DP && !a.mask)
+    launch<DP, true, false>(a, d, items, stream);
+  else if (a.cache.dim == DP)
+    launch<DP, true, true>(a, d, items, stream);
+  else if (!a.mask)
+    launch<DP, false, false>(a, d, items, stream);
   else
-    hipLaunchKernelGGL((attend_kernel<DP, false>), grid, dim3(kThreads), 0, stream, a, d, items);
-  launched("attention");
-  if (!d.sums) return;
-  const int64_t rows = a.n * a.q_heads;
-  hipLaunchKernelGGL(join_kernel<DP>, dim3(static_cast<unsigned>(std::min(rows, kMaxGrid))), dim3(kThreads), 0, stream, a, d, rows);
-  launched("attention's join");
+    launch<DP, false, true>(a, d, items, stream);
 }
 
 }  // namespace
 
 size_t decode_attend_workspace(int64_t n, int q_heads, int heads, int dim, int64_t max_length, int64_t window) {
   const Parts d = parts_of(n, q_heads, heads, dim, max_length, window, nullptr);
-  return d.parts > 1 ? static_cast<size_t>(n) * q_heads * d.parts * (static_cast<size_t>(dim) * 4 + 8) : 0;
+  return d.pieces > 1 ? static_cast<size_t>(n) * q_heads * d.pieces * (static_cast<size_t>(dim) * 4 + 8) : 0;
 }
 
 bool decode_attend(const AttendArgs& a, hipStream_t stream) {
   const Parts d = parts_of(a.n, a.q_heads, a.cache.heads, a.cache.dim, a.max_length, a.window, a.workspace);
   const int64_t groups = a.n * a.cache.heads * d.blocks;        // (n * q_heads fits 32 bits, so do these)
-  if (groups * d.parts >= int64_t(1) << 31) return false;
-  const uint32_t items = static_cast<uint32_t>(groups * d.parts);
+  if (groups * d.pieces >= int64_t(1) << 31 || a.n * a.q_heads * ((a.cache.dim + 63) / 64) >= int64_t(1) << 31) return false;
+  const uint32_t items = static_cast<uint32_t>(groups * d.pieces);
   if (a.cache.dim <= 64)
     launch<64>(a, d, items, stream);
   else if (a.cache.dim <= 128)
     launch<128>(a, d, items, stream);
   else
     launch<256>(a, d, items, stream);
+  if (!d.sums) return true;
+  const uint32_t joins = static_cast<uint32_t>(a.n * a.q_heads) * ((a.cache.dim + 63) / 64);
+  for (uint32_t base = 0; base < joins; base += kMaxGrid) {
+    const dim3 grid(std::min(joins - base, kMaxGrid));
+    const dim3 threads(kThreads);
+    if (d.keys == kStretchKeys)
+      hipLaunchKernelGGL((join_kernel<1, false>), grid, threads, 0, stream, a, d, base);
+    else if (d.keys == kRunKeys)
+      hipLaunchKernelGGL((join_kernel<kFour, false>), grid, threads, 0, stream, a, d, base);
+    else if (d.keys == 256)
+      hipLaunchKernelGGL((join_kernel<2, true>), grid, threads, 0, stream, a, d, base);
+    else
+      hipLaunchKernelGGL((join_kernel<4, true>), grid, threads, 0, stream, a, d, base);
+    launched("attention's join");
+  }
   return true;
 }
 

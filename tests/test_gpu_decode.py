@@ -327,19 +327,29 @@ def test_attend_infinite_values(de):
     within(out[fine], want[0][fine], bound[0][fine])
 
 
-def test_attend_company_leaves_bits(de):
+@pytest.mark.parametrize("n, heads, q_heads, dim, most, page, window", [
+    (40, 2, 8, 128, 100, 16, 0), (40, 2, 8, 128, 5000, 64, 0), (400, 1, 2, 64, 5000, 64, 0), (700, 2, 2, 64, 700, 8, 0), (90, 4, 20, 256, 7000, 32, 0),
+    (300, 2, 2, 72, 4500, 128, 4200), (48, 8, 8, 64, 33000, 256, 0), (64, 2, 66, 128, 9000, 64, 0)])
+def test_attend_company_leaves_bits(de, n, heads, q_heads, dim, most, page, window):
     """A row's bits do not depend on the other rows, on the page order or on what is behind its keys."""
-    g = gen(15)
-    for n_keys, page in ((100, 16), (5000, 64)):
-        cache, tables = paged(g, [n_keys] * 40, 2, page, 128, garbage=1.0)
-        for t in cache:
-            t.copy_(normal(g, *t.shape).to(B))
-        q = normal(g, 40, 1024).to(B)
-        lengths = torch.randint(1, n_keys + 1, (40,), generator=g, device="cuda").int()
-        all_rows = de.attend(q, cache, tables, lengths)
-        for r in (0, 17, 39):
-            assert torch.equal(de.attend(q[r:r + 1], cache, tables[r:r + 1], lengths[r:r + 1])[0], all_rows[r])
-        assert torch.equal(de.attend(q, cache, tables, lengths), all_rows)
+    g = gen(15 + n)
+    per = -(-most // page)
+    pages = max(4 * per, 64)
+    cache = de.Cache(*(normal(g, pages, heads, page, dim).to(B) for _ in range(2)))
+    tables = torch.randint(0, pages, (n, per), generator=g, device="cuda").int()       # (rows may share pages)
+    q = normal(g, n, q_heads * dim).to(B)
+    lengths = torch.randint(1, most + 1, (n,), generator=g, device="cuda").int()
+    lengths[0], lengths[n // 2] = most, 0
+    all_rows = de.attend(q, cache, tables, lengths, window=window)
+    assert torch.equal(de.attend(q, cache, tables, lengths, window=window), all_rows)
+    for first, last in ((0, 1), (n // 3, n // 3 + 1), (n - 1, n), (n // 2, n // 2 + 2), (1, 1 + n // 5)):
+        some = de.attend(q[first:last], cache, tables[first:last], lengths[first:last], window=window)
+        assert torch.equal(some, all_rows[first:last]), (first, last)
+    swapped = torch.randperm(pages, generator=g, device="cuda")
+    moved = de.Cache(*(torch.empty_like(t) for t in cache))
+    for a, b in zip(moved, cache):
+        a[swapped] = b
+    assert torch.equal(de.attend(q, moved, swapped[tables.long()].int(), lengths, window=window), all_rows)
 
 
 def test_attend_far_offsets(de):
