@@ -3,9 +3,8 @@
 //
 // log softmax only shifts a beam's logits, so a beam's best candidates are those of its
 // logits.  A workgroup takes a segment of a row into registers: sum of exponentials
-// around its maximum, and its k largest.  The least of the four waves' ceil(k / 4)-th largest of
-// their lanes' maxima (to 16 bits, rounded down) is a bound that k values reach and few others; those that
-// reach it go to LDS and are ranked by counting the larger ones.  Where more reach it than LDS
+// around its maximum, and its k largest.  From the lanes' maxima comes a bound that k values reach
+// and few others; those that reach it go to LDS and are ranked by counting the larger ones.  Where more reach it than LDS
 // holds (a row of equal values) the k are taken one after the other.  A second kernel sums a beam's segments, in order, and
 // takes the k largest of the segments' lists the same way.
 //
@@ -52,19 +51,16 @@ struct Chosen {                        // in LDS
 };
 
 // A bound that k of the workgroup's values reach if v is each lane's largest; -inf where fewer lanes are
-// open.  All threads call it; what was written to LDS before is visible after it.
+// open: the larger of two such, the least of the waves' ceil(k / 4)-th largest (close where the waves are alike) and the
+// largest of their k-th (where one has most of them).  All threads call it; what was written to LDS before is visible
+// after it.
 __device__ __forceinline__ float bound_of_all(Chosen& s, float v, int k) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float own = bound_of(v, (k + kWaves - 1) / kWaves);
-  if (lane == 0) s.bounds[0][wave] = own;
+  const float share = bound_of(v, (k + kWaves - 1) / kWaves), alone = bound_of(v, k);
+  if (lane == 0) s.bounds[0][wave] = share, s.bounds[1][wave] = alone;
   __syncthreads();
-  const float least = fminf(fminf(s.bounds[0][0], s.bounds[0][1]), fminf(s.bounds[0][2], s.bounds[0][3]));
-  if (least > kClosed) return least;
-  // a wave with fewer open lanes than its share: the best wave's k-th
-  const float single = bound_of(v, k);
-  if (lane == 0) s.bounds[1][wave] = single;
-  __syncthreads();
-  return fmaxf(fmaxf(s.bounds[1][0], s.bounds[1][1]), fmaxf(s.bounds[1][2], s.bounds[1][3]));
+  return fmaxf(fminf(fminf(s.bounds[0][0], s.bounds[0][1]), fminf(s.bounds[0][2], s.bounds[0][3])),
+               fmaxf(fmaxf(s.bounds[1][0], s.bounds[1][1]), fmaxf(s.bounds[1][2], s.bounds[1][3])));
 }
 
 // The k largest of the candidates in `s`: rank r's key to put(r, key), r below the number of them and k.
@@ -94,174 +90,242 @@ struct Segments {
   uint64_t* lists;                     // [row][segment][k] keys, largest first, 0 past the last
 };
 
+// the wave's largest, in all lanes
+__device__ __forceinline__ float wave_top(float v) {
+  v = fmaxf(v, rotate16<8>(v));
+  v = fmaxf(v, rotate16<4>(v));
+  v = fmaxf(v, rotate16<2>(v));
+  v = fmaxf(v, rotate16<1>(v));
+  return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+
 // V: groups of 8 values per lane
 template <bool F32, int V>
-__global__ __launch_bounds__(kThreads) void segment_kernel(BeamArgs p, Segments g, int64_t items) {
+__global__ __launch_bounds__(kThreads) void segment_kernel(BeamArgs p, Segments g, uint32_t base) {
   __shared__ Chosen s;
   __shared__ float2 waves[kWaves];
+  // W consecutive values per lane and request (16 bytes), `kThreads * W` further on the next
+  constexpr int kSize = kThreads * 8 * V, W = F32 ? 4 : 8, kBytes = F32 ? 4 : 2;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t row = item / g.count;
-    const int segment = static_cast<int>(item - row * g.count);
-    // beams without candidates of their own are not read
-    const float score = p.scores[row];
-    if ((p.ended && p.ended[row]) || !(score > kClosed)) continue;        // (the same for the whole workgroup; the second kernel skips them too)
-    if (threadIdx.x == 0) s.count = 0;
-    const char* base = static_cast<const char*>(p.logits) + row * p.ldl * (F32 ? 4 : 2);
-    const int first = segment * (kThreads * 8 * V) + 8 * threadIdx.x;
-    float v[8 * V];
+  const uint32_t item = base + blockIdx.x;
+  const uint32_t row = item / g.count;
+  const int start = static_cast<int>(item - row * g.count) * kSize, first = start + W * threadIdx.x;
+  auto index = [&](int i) { return first + i / W * (kThreads * W) + i % W; };
+  const char* from = static_cast<const char*>(p.logits) + (static_cast<int64_t>(row) * p.ldl + first) * kBytes;
+  float v[8 * V];
+  if (start + kSize <= p.words) {                      // (all requests at once, no tests between them)
+    uint4 raw[8 * V / W];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int at = first + i * kThreads * 8;
-      read8<F32>(base + static_cast<int64_t>(at) * (F32 ? 4 : 2), min(8, max(0, p.words - at)), v + 8 * i);
+    for (int i = 0; i < 8 * V / W; ++i) raw[i] = load16(from + i * kThreads * 16);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)                    // NaN is closed, +infinity the largest finite value
-        v[8 * i + j] = at + j < p.words ? fminf(fmaxf(v[8 * i + j], kClosed), kLargest) : kClosed;
-    }
-    float top = v[0];
+    for (int i = 0; i < 8 * V / W; ++i) {
+      const uint32_t e[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
-    for (int i = 1; i < 8 * V; ++i) top = fmaxf(top, v[i]);
-    float m = top;
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) m = fmaxf(m, __shfl_xor(m, w));
-    const float around = m == kClosed ? 0.f : m;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8 * V; ++i) sum += __builtin_amdgcn_exp2f((v[i] - around) * kLog2e);
-    sum = wave_sum(sum);
-    if (lane == 0) waves[wave] = make_float2(m, sum);
-    const float bound = bound_of_all(s, top, p.k);
-    if (threadIdx.x == 0) {
-      const float all = fmaxf(fmaxf(waves[0].x, waves[1].x), fmaxf(waves[2].x, waves[3].x)), base2 = all == kClosed ? 0.f : all;
-      float total = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) total += __builtin_amdgcn_exp2f((waves[w].x - base2) * kLog2e) * waves[w].y;
-      g.state[item] = make_float2(all, total);
-    }
-    if (top >= bound) {
-#pragma unroll
-      for (int i = 0; i < 8 * V; ++i)
-        if (v[i] >= bound && v[i] > kClosed) {
-          const int at = atomicAdd(&s.count, 1);
-          if (at < kRoom) s.keys[at] = key_of(v[i], first + i / 8 * (kThreads * 8) + i % 8);
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (F32) {
+          v[4 * i + j] = __uint_as_float(e[j]);
+        } else {
+          v[8 * i + 2 * j] = __uint_as_float(e[j] << 16);
+          v[8 * i + 2 * j + 1] = __uint_as_float(e[j] & 0xffff0000u);
         }
-    }
-    __syncthreads();
-    uint64_t* list = g.lists + item * p.k;
-    if (s.count <= kRoom) {
-      rank_all(s, p.k, [&](int rank, uint64_t key) { list[rank] = key; });
-      for (int i = s.count + threadIdx.x; i < p.k; i += kThreads) list[i] = 0;
-    } else {
-      uint64_t before = ~uint64_t(0);
-      for (int round = 0; round < p.k; ++round) {
-        uint64_t best = 0;
-#pragma unroll
-        for (int i = 0; i < 8 * V; ++i) {
-          const uint64_t key = key_of(v[i], first + i / 8 * (kThreads * 8) + i % 8);
-          best = key < before && key > best ? key : best;
-        }
-        best = wave_max(best);
-        if (lane == 0) s.best[wave] = best;
-        __syncthreads();
-        best = max(max(s.best[0], s.best[1]), max(s.best[2], s.best[3]));
-        if (threadIdx.x == 0) list[round] = best;
-        before = best;
-        __syncthreads();
       }
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8 * V; ++i) {
+      v[i] = kClosed;
+      const char* at = from + (i / W * (kThreads * W) + i % W) * kBytes;
+      if (index(i) < p.words) v[i] = F32 ? *reinterpret_cast<const float*>(at) : bf2f(*reinterpret_cast<const uint16_t*>(at));
+    }
+  }
+  if (threadIdx.x == 0) s.count = 0;
+  // beams without candidates of their own: the second kernel skips them too
+  const float score = p.scores[row];
+  if ((p.ended && p.ended[row]) || !(score > kClosed)) return;     // (the same for the whole workgroup)
+#pragma unroll
+  for (int i = 0; i < 8 * V; ++i) v[i] = fminf(fmaxf(v[i], kClosed), kLargest);     // NaN is closed, +infinity the largest finite value
+  float top = v[0];
+#pragma unroll
+  for (int i = 1; i < 8 * V; ++i) top = fmaxf(top, v[i]);
+  const float m = wave_top(top), around = m == kClosed ? 0.f : m;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8 * V; ++i) sum += __builtin_amdgcn_exp2f((v[i] - around) * kLog2e);
+  sum = wave_sum(sum);
+  if (lane == 0) waves[wave] = make_float2(m, sum);
+  const float bound = bound_of_all(s, top, p.k);
+  if (threadIdx.x == 0) {
+    const float all = fmaxf(fmaxf(waves[0].x, waves[1].x), fmaxf(waves[2].x, waves[3].x)), base2 = all == kClosed ? 0.f : all;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total += __builtin_amdgcn_exp2f((waves[w].x - base2) * kLog2e) * waves[w].y;
+    g.state[item] = make_float2(all, total);
+  }
+  if (__any(top >= bound)) {
+#pragma unroll
+    for (int i = 0; i < 8 * V; ++i)
+      if (__any(v[i] >= bound)) {                      // (few: most are one comparison for the wave)
+        if (v[i] >= bound && v[i] > kClosed) {
+          const int at = atomicAdd(&s.count, 1);
+          if (at < kRoom) s.keys[at] = key_of(v[i], index(i));
+        }
+      }
+  }
+  __syncthreads();
+  uint64_t* list = g.lists + static_cast<int64_t>(item) * p.k;
+  if (s.count <= kRoom) {
+    rank_all(s, p.k, [&](int rank, uint64_t key) { list[rank] = key; });
+    for (int i = s.count + threadIdx.x; i < p.k; i += kThreads) list[i] = 0;
+    return;
+  }
+  uint64_t before = ~uint64_t(0);
+  for (int round = 0; round < p.k; ++round) {
+    uint64_t best = 0;
+#pragma unroll
+    for (int i = 0; i < 8 * V; ++i) {
+      const uint64_t key = key_of(v[i], index(i));
+      best = key < before && key > best ? key : best;
+    }
+    best = wave_max(best);
+    if (lane == 0) s.best[wave] = best;
+    __syncthreads();
+    best = max(max(s.best[0], s.best[1]), max(s.best[2], s.best[3]));
+    if (threadIdx.x == 0) list[round] = best;
+    before = best;
     __syncthreads();
   }
 }
 
-// One sequence: its beams' sums, then the k largest of all lists.
+// One sequence: its beams' sums, then the k largest of all lists.  FLAT: a thread keeps up to kFlat of the lists' entries,
+// requested at once; else it walks along the lists.
+constexpr int kFlat = 8;
+template <bool FLAT>
 __global__ __launch_bounds__(kThreads) void choose_kernel(BeamArgs p, Segments g) {
   __shared__ Chosen s;
   __shared__ float2 shift[kBeamMaxBeams];      // a beam's largest logit, and the value of that one; -inf: none of its logits
   __shared__ float kept[kBeamMaxBeams];        // an ended beam's score, -inf: it has not ended
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t b = blockIdx.x; b < p.sequences; b += gridDim.x) {
-    if (threadIdx.x == 0) s.count = 0;
-    for (int w = wave; w < p.beams; w += kWaves) {
-      const int64_t row = b * p.beams + w;
-      const float given = p.scores[row], score = fminf(given, kLargest);
-      const bool open = given > kClosed, over = p.ended && p.ended[row];
-      float m = kClosed, total = 0.f;
-      if (open && !over) {
-        const float2* state = g.state + row * g.count;
-        for (int i = lane; i < g.count; i += 64) m = fmaxf(m, state[i].x);
+  const int64_t b = blockIdx.x;
+  const int lists = p.beams * g.count, entries = lists * p.k;
+  const uint64_t* all = g.lists + b * entries;
+  uint64_t own[FLAT ? kFlat : 1];
+  if constexpr (FLAT) {
+    // The lists' first entries first, so that every wave has some of them.  (Of a beam without candidates the entries are
+    // whatever the workspace held; they are not used.)
 #pragma unroll
-        for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-        if (m > kClosed)
-          for (int i = lane; i < g.count; i += 64) total += __builtin_amdgcn_exp2f((state[i].x - m) * kLog2e) * state[i].y;
-        total = wave_sum(total);
-      }
-      if (lane == 0) {
-        shift[w] = make_float2(m, score - logf(total));
-        kept[w] = open && over ? score : kClosed;
-      }
+    for (int j = 0; j < kFlat; ++j) {
+      const int i = threadIdx.x + j * kThreads;
+      own[j] = 0;
+      if (j * kThreads < entries && i < entries) own[j] = all[i % lists * p.k + i / lists];
     }
-    __syncthreads();
-    // candidates' keys: a thread's lists are threadIdx.x, + 256, ...
-    const int lists = p.beams * g.count;
-    const uint64_t* all = g.lists + b * lists * p.k;
-    auto key_at = [&](int list, int i) -> uint64_t {
-      const int w = list / g.count;
-      if (shift[w].x == kClosed) return 0;
-      const uint64_t key = all[static_cast<int64_t>(list) * p.k + i];
-      // (a sum past the least finite value is closed, as -infinity is)
-      return key ? key_of((value_of(static_cast<uint32_t>(key >> 32)) - shift[w].x) + shift[w].y, w * p.words + index_of(key)) : 0;
-    };
-    uint64_t head = 0;
+  }
+  if (threadIdx.x == 0) s.count = 0;
+  // 16 lanes per beam
+  const int part = threadIdx.x & 15;
+  for (int w = threadIdx.x >> 4; w < p.beams; w += kThreads / 16) {
+    const int64_t row = b * p.beams + w;
+    const float given = p.scores[row], score = fminf(given, kLargest);
+    const bool open = given > kClosed, over = p.ended && p.ended[row], reads = open && !over;
+    const float2* state = g.state + row * g.count;
+    float2 one[2];                             // (its first ones, requested at once)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      one[j] = make_float2(kClosed, 0.f);
+      if (part + 16 * j < g.count) one[j] = state[part + 16 * j];
+      if (!reads) one[j] = make_float2(kClosed, 0.f);
+    }
+    float m = fmaxf(one[0].x, one[1].x);
+    for (int i = part + 32; i < g.count && reads; i += 16) m = fmaxf(m, state[i].x);
+    m = fmaxf(m, rotate16<8>(m));
+    m = fmaxf(m, rotate16<4>(m));
+    m = fmaxf(m, rotate16<2>(m));
+    m = fmaxf(m, rotate16<1>(m));
+    float total = 0.f;
+    if (m > kClosed) {
+      total = __builtin_amdgcn_exp2f((one[0].x - m) * kLog2e) * one[0].y + __builtin_amdgcn_exp2f((one[1].x - m) * kLog2e) * one[1].y;
+      for (int i = part + 32; i < g.count; i += 16) total += __builtin_amdgcn_exp2f((state[i].x - m) * kLog2e) * state[i].y;
+    }
+    total = sum16(total);
+    if (part == 0) {
+      shift[w] = make_float2(m, score - logf(total));
+      kept[w] = open && over ? score : kClosed;
+    }
+  }
+  __syncthreads();
+  // (a sum past the least finite value is closed, as -infinity is)
+  auto valued = [&](uint64_t key, int w) -> uint64_t {
+    if (!key || shift[w].x == kClosed) return 0;
+    return key_of((value_of(static_cast<uint32_t>(key >> 32)) - shift[w].x) + shift[w].y, w * p.words + index_of(key));
+  };
+  auto key_at = [&](int list, int i) {           // (a list of a closed beam is not read)
+    const int w = list / g.count;
+    return shift[w].x == kClosed ? uint64_t(0) : valued(all[static_cast<int64_t>(list) * p.k + i], w);
+  };
+  uint64_t head = 0;
+  if constexpr (FLAT) {
+#pragma unroll
+    for (int j = 0; j < kFlat; ++j) {
+      const int i = threadIdx.x + j * kThreads;
+      if (j * kThreads < entries && i < entries) own[j] = valued(own[j], i % lists / g.count);
+      head = max(head, own[j]);
+    }
+  } else {
     for (int i = threadIdx.x; i < lists; i += kThreads) head = max(head, key_at(i, 0));
-    if (threadIdx.x < p.beams && kept[threadIdx.x] > kClosed)
-      head = max(head, key_of(kept[threadIdx.x], threadIdx.x * p.words + p.end));
-    const float bound = bound_of_all(s, head ? value_of(static_cast<uint32_t>(head >> 32)) : kClosed, p.k);
-    auto each = [&](auto&& f) {                      // the thread's candidates that reach the bound
+  }
+  const uint64_t ended = threadIdx.x < p.beams && kept[threadIdx.x] > kClosed ? key_of(kept[threadIdx.x], threadIdx.x * p.words + p.end) : 0;
+  head = max(head, ended);
+  const float bound = bound_of_all(s, head ? value_of(static_cast<uint32_t>(head >> 32)) : kClosed, p.k);
+  auto reaches = [&](uint64_t key) { return key && !(value_of(static_cast<uint32_t>(key >> 32)) < bound); };
+  auto each = [&](auto&& f) {                      // the thread's candidates that reach the bound
+    if constexpr (FLAT) {
+#pragma unroll
+      for (int j = 0; j < kFlat; ++j)
+        if (reaches(own[j])) f(own[j]);
+    } else {
       for (int i = threadIdx.x; i < lists; i += kThreads)
         for (int j = 0; j < p.k; ++j) {
           const uint64_t key = key_at(i, j);
-          if (!key || value_of(static_cast<uint32_t>(key >> 32)) < bound) break;
+          if (!reaches(key)) break;
           f(key);
         }
-      if (threadIdx.x < p.beams && kept[threadIdx.x] > kClosed) f(key_of(kept[threadIdx.x], threadIdx.x * p.words + p.end));
-    };
-    each([&](uint64_t key) {
-      const int at = atomicAdd(&s.count, 1);
-      if (at < kRoom) s.keys[at] = key;
-    });
-    __syncthreads();
-    auto put = [&](int rank, uint64_t key) {
-      const int64_t at = b * p.k + rank;
-      if (!key) {
-        p.parents[at] = p.tokens[at] = -1;
-        p.new_scores[at] = kClosed;
-        p.new_ended[at] = 0;
-        return;
-      }
-      const uint32_t index = index_of(key);
-      const int w = static_cast<int>(index / p.words), word = static_cast<int>(index - w * p.words);
-      p.parents[at] = static_cast<int32_t>(b * p.beams + w);
-      p.tokens[at] = word;
-      p.new_scores[at] = value_of(static_cast<uint32_t>(key >> 32));
-      p.new_ended[at] = word == p.end || kept[w] > kClosed;
-    };
-    if (s.count <= kRoom) {
-      rank_all(s, p.k, put);
-      for (int i = s.count + threadIdx.x; i < p.k; i += kThreads) put(i, 0);
-    } else {
-      uint64_t before = ~uint64_t(0);
-      for (int round = 0; round < p.k; ++round) {
-        uint64_t best = 0;
-        each([&](uint64_t key) { best = key < before && key > best ? key : best; });
-        best = wave_max(best);
-        if (lane == 0) s.best[wave] = best;
-        __syncthreads();
-        best = max(max(s.best[0], s.best[1]), max(s.best[2], s.best[3]));
-        if (threadIdx.x == 0) put(round, best);
-        before = best;
-        __syncthreads();
-      }
     }
+    if (ended) f(ended);
+  };
+  each([&](uint64_t key) {
+    const int at = atomicAdd(&s.count, 1);
+    if (at < kRoom) s.keys[at] = key;
+  });
+  __syncthreads();
+  auto put = [&](int rank, uint64_t key) {
+    const int64_t at = b * p.k + rank;
+    if (!key) {
+      p.parents[at] = p.tokens[at] = -1;
+      p.new_scores[at] = kClosed;
+      p.new_ended[at] = 0;
+      return;
+    }
+    const uint32_t index = index_of(key);
+    const int w = static_cast<int>(index / p.words), word = static_cast<int>(index - w * p.words);
+    p.parents[at] = static_cast<int32_t>(b * p.beams + w);
+    p.tokens[at] = word;
+    p.new_scores[at] = value_of(static_cast<uint32_t>(key >> 32));
+    p.new_ended[at] = word == p.end || kept[w] > kClosed;
+  };
+  if (s.count <= kRoom) {
+    rank_all(s, p.k, put);
+    for (int i = s.count + threadIdx.x; i < p.k; i += kThreads) put(i, 0);
+    return;
+  }
+  uint64_t before = ~uint64_t(0);
+  for (int round = 0; round < p.k; ++round) {
+    uint64_t best = 0;
+    each([&](uint64_t key) { best = key < before && key > best ? key : best; });
+    best = wave_max(best);
+    if (lane == 0) s.best[wave] = best;
+    __syncthreads();
+    best = max(max(s.best[0], s.best[1]), max(s.best[2], s.best[3]));
+    if (threadIdx.x == 0) put(round, best);
+    before = best;
     __syncthreads();
   }
 }
@@ -270,7 +334,16 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(BeamArgs p, Segments g
 int groups_of(int words) { return words <= 65536 ? 2 : 4; }
 int segments_of(int words) { return (words + kThreads * 8 * groups_of(words) - 1) / (kThreads * 8 * groups_of(words)); }
 
-constexpr int64_t kMaxGrid = int64_t(1) << 22;
+// workgroups of a launch (a grid counts fewer than 2^32 threads)
+constexpr uint32_t kMaxGrid = 1u << 23;
+
+template <bool F32, int V>
+void segments(const BeamArgs& a, const Segments& g, uint32_t items, hipStream_t stream) {
+  for (uint32_t base = 0; base < items; base += kMaxGrid) {
+    hipLaunchKernelGGL((segment_kernel<F32, V>), dim3(std::min(items - base, kMaxGrid)), dim3(kThreads), 0, stream, a, g, base);
+    launched("choice of tokens, segments");
+  }
+}
 
 }  // namespace
 
@@ -281,21 +354,23 @@ size_t decode_beam_workspace(int64_t sequences, int beams, int words, int k) {
 void decode_beam(const BeamArgs& a, hipStream_t stream) {
   Segments g;
   g.count = segments_of(a.words);
-  const int64_t items = a.sequences * a.beams * g.count;
+  const uint32_t items = static_cast<uint32_t>(a.sequences * a.beams * g.count);     // (below 2^24 rows of at most 128)
   g.lists = static_cast<uint64_t*>(a.workspace);
-  g.state = reinterpret_cast<float2*>(g.lists + items * a.k);
-  const dim3 grid(static_cast<unsigned>(std::min(items, kMaxGrid))), threads(kThreads);
+  g.state = reinterpret_cast<float2*>(g.lists + static_cast<int64_t>(items) * a.k);
   const bool four = groups_of(a.words) == 4;
   if (a.f32 && four)
-    hipLaunchKernelGGL((segment_kernel<true, 4>), grid, threads, 0, stream, a, g, items);
+    segments<true, 4>(a, g, items, stream);
   else if (a.f32)
-    hipLaunchKernelGGL((segment_kernel<true, 2>), grid, threads, 0, stream, a, g, items);
+    segments<true, 2>(a, g, items, stream);
   else if (four)
-    hipLaunchKernelGGL((segment_kernel<false, 4>), grid, threads, 0, stream, a, g, items);
+    segments<false, 4>(a, g, items, stream);
   else
-    hipLaunchKernelGGL((segment_kernel<false, 2>), grid, threads, 0, stream, a, g, items);
-  launched("choice of tokens, segments");
-  hipLaunchKernelGGL(choose_kernel, dim3(static_cast<unsigned>(std::min(a.sequences, kMaxGrid))), threads, 0, stream, a, g);
+    segments<false, 2>(a, g, items, stream);
+  const dim3 grid(static_cast<unsigned>(a.sequences)), threads(kThreads);
+  if (static_cast<int64_t>(a.beams) * g.count * a.k <= kFlat * kThreads)
+    hipLaunchKernelGGL(choose_kernel<true>, grid, threads, 0, stream, a, g);
+  else
+    hipLaunchKernelGGL(choose_kernel<false>, grid, threads, 0, stream, a, g);
   launched("choice of tokens");
 }
 

@@ -1,5 +1,4 @@
-// Device helpers of the decoding operators: eight values of a row at a time,
-// and the way from a token's place to its page.
+// Device helpers of the decoding operators: 16 bytes of a row at a time, and the way from a token's place to its page.
 #pragma once
 
 #include "decode.hpp"
@@ -8,47 +7,49 @@
 namespace dycl {
 namespace k {
 
-// 8 consecutive values of bf16 or float32 from any element on; only the first
-// `count` of fewer than 8 are read (the others are 0)
+// What a lane moves at a time: 16 bytes of values
 template <bool F32>
-__device__ __forceinline__ void read8(const void* p, int count, float* f) {
-  if (count >= 8) {
-    if constexpr (F32) {
-      const uint4 a = load16(p), b = load16(static_cast<const char*>(p) + 16);
-      const uint32_t e[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+constexpr int kWide = F32 ? 4 : 8;
+
+// N consecutive values (8 of bf16, 4 of either) from any element on; only the first `count` of fewer
+// are read (the others are 0)
+template <bool F32, int N>
+__device__ __forceinline__ void read_values(const void* p, int count, float* f) {
+  static_assert(F32 ? N == 4 : N == 8, "16 bytes");
+  if (count >= N) {
+    const uint4 a = load16(p);
+    const uint32_t e[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(e[j]);
-    } else {
-      const uint4 a = load16(p);
-      const uint32_t e[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (F32) {
+        f[j] = __uint_as_float(e[j]);
+      } else {
         f[2 * j] = __uint_as_float(e[j] << 16);
         f[2 * j + 1] = __uint_as_float(e[j] & 0xffff0000u);
       }
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < N; ++j) {
       f[j] = 0.f;
       if (j < count) f[j] = F32 ? static_cast<const float*>(p)[j] : bf2f(static_cast<const uint16_t*>(p)[j]);
     }
   }
 }
 
-template <bool F32>
-__device__ __forceinline__ void write8(void* p, int count, const float* f) {
-  if (count >= 8) {
-    if constexpr (F32) {
+template <bool F32, int N>
+__device__ __forceinline__ void write_values(void* p, int count, const float* f) {
+  typedef uint32_t bits64 __attribute__((ext_vector_type(2), aligned(2)));
+  if (count >= N) {
+    if constexpr (F32)
       store16(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
-      store16(static_cast<char*>(p) + 16,
-              make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
-    } else {
+    else if constexpr (N == 8)
       store16(p, make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])));
-    }
+    else
+      *static_cast<bits64*>(p) = bits64{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
   } else {
 #pragma unroll
-    for (int j = 0; j < 7; ++j) {
+    for (int j = 0; j < N - 1; ++j) {
       if (j >= count) continue;
       if constexpr (F32)
         static_cast<float*>(p)[j] = f[j];

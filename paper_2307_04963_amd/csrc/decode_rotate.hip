@@ -6,10 +6,10 @@
 // it is reduced to an eighth of a turn around the nearest quarter; sine and cosine of
 // that are Taylor polynomials in float32 (remainders below 2^-28 at pi / 4).
 //
-// Bound by HBM: every value is read and written once.  A workgroup takes a tile of rows;
+// Bound by HBM: every value is read and written once (measured: 251 MB of float32 41 us, 6.1 TB/s; prompts of 6000
+// rows into the cache, 157 MB, 26 us; one token of 32 heads 2.2 us, a launch).  A workgroup takes a tile of rows;
 // their cosines and sines are made once into LDS for all of a row's heads, then a lane
-// takes eight pairs (16 bytes of each half in bf16, at any alignment) or eight
-// neighbours.
+// takes 16 bytes (of each half, or of neighbours), at any alignment.
 #include "decode_dev.hpp"
 
 namespace dycl {
@@ -51,8 +51,19 @@ struct Units {
   int rows;                      // of a tile
   int turned, copied, plain;     // units of a head's turned and other values, of a head of v
   int of_q, of_row;              // units of q's heads, of a whole row
-  Divide row, head, v_head;
+  Divide row, head, v_head, pair;
 };
+
+// cosines and sines of a tile's rows
+__device__ __forceinline__ void make_table(const RotateArgs& p, const Units& u, int64_t r0, int rows, float2* table) {
+  for (int i = threadIdx.x; i < rows * p.pairs; i += kThreads) {
+    const int r = u.pair(i);
+    float2 cs = turn(p.positions[r0 + r], p.frequencies[i - r * p.pairs]);
+    cs.x *= p.magnitude;
+    cs.y *= p.magnitude * p.sign;
+    table[i] = cs;
+  }
+}
 
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs p, Units u) {
@@ -60,7 +71,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs p, Units u)
   __shared__ int64_t pages[kMaxRows];          // page of the row's token, -1: none
   __shared__ int32_t places[kMaxRows];
   const int t = threadIdx.x, per_head = u.turned + u.copied;
-  const size_t size = F32 ? 4 : 2;
+  constexpr size_t size = F32 ? 4 : 2;
+  constexpr int W = kWide<F32>;
   for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * u.rows; r0 < p.n; r0 += static_cast<int64_t>(gridDim.x) * u.rows) {
     const int rows = static_cast<int>(min(p.n - r0, static_cast<int64_t>(u.rows)));
     for (int r = t; r < rows; r += kThreads) {
@@ -68,13 +80,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs p, Units u)
       places[r] = at;
       pages[r] = p.k ? page_of(p.cache, p.sequence ? p.sequence[r0 + r] : r0 + r, at) : -1;
     }
-    for (int i = t; i < rows * p.pairs; i += kThreads) {
-      const int r = i / p.pairs;
-      float2 cs = turn(p.positions[r0 + r], p.frequencies[i - r * p.pairs]);
-      cs.x *= p.magnitude;
-      cs.y *= p.magnitude * p.sign;
-      table[i] = cs;
-    }
+    make_table(p, u, r0, rows, table);
     __syncthreads();
     for (int i = t; i < rows * u.of_row; i += kThreads) {
       const int r = u.row(i);
@@ -109,57 +115,167 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs p, Units u)
         turned = !is_v && w < u.turned;
         if (is_v) w += u.turned;               // (counted as copied from the head's first value)
         first = is_v ? 0 : 2 * p.pairs;
-        first += 8 * (w - u.turned);
+        first += W * (w - u.turned);
       }
-      if (!to_cache) first = 2 * p.pairs + 8 * (w - u.turned);
-      float a[8], b[8];
+      if (!to_cache) first = 2 * p.pairs + W * (w - u.turned);
+      float a[W], b[W];
       if (!turned) {
-        count = min(8, p.dim - first);
-        read8<F32>(from + first * size, count, a);
+        count = min(W, p.dim - first);
+        read_values<F32, W>(from + first * size, count, a);
         if (to_cache)
-          write8<false>(to + first * 2, count, a);
+          write_values<false, W>(to + first * 2, count, a);
         else {
           if (p.padding && places[r] < 0)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) a[j] = 0.f;
-          write8<F32>(to + first * size, count, a);
+            for (int j = 0; j < W; ++j) a[j] = 0.f;
+          write_values<F32, W>(to + first * size, count, a);
         }
         continue;
       }
       const bool none = !to_cache && p.padding && places[r] < 0;
       const float2* cs = table + r * p.pairs;
       if (p.interleaved) {
-        first = 8 * w;
-        count = min(8, 2 * p.pairs - first);
-        read8<F32>(from + first * size, count, a);
+        first = W * w;
+        count = min(W, 2 * p.pairs - first);
+        read_values<F32, W>(from + first * size, count, a);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 c = cs[min(4 * w + j, p.pairs - 1)];
+        for (int j = 0; j < W / 2; ++j) {
+          const float2 c = cs[min(W / 2 * w + j, p.pairs - 1)];
           b[2 * j] = none ? 0.f : a[2 * j] * c.x - a[2 * j + 1] * c.y;
           b[2 * j + 1] = none ? 0.f : a[2 * j + 1] * c.x + a[2 * j] * c.y;
         }
         if (to_cache)
-          write8<false>(to + first * 2, count, b);
+          write_values<false, W>(to + first * 2, count, b);
         else
-          write8<F32>(to + first * size, count, b);
+          write_values<F32, W>(to + first * size, count, b);
       } else {
-        first = 8 * w;
-        count = min(8, p.pairs - first);
-        read8<F32>(from + first * size, count, a);
-        read8<F32>(from + (p.pairs + first) * size, count, b);
+        first = W * w;
+        count = min(W, p.pairs - first);
+        read_values<F32, W>(from + first * size, count, a);
+        read_values<F32, W>(from + (p.pairs + first) * size, count, b);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < W; ++j) {
           const float2 c = cs[min(first + j, p.pairs - 1)];
           const float y = a[j] * c.x - b[j] * c.y;
           b[j] = none ? 0.f : b[j] * c.x + a[j] * c.y;
           a[j] = none ? 0.f : y;
         }
         if (to_cache) {
-          write8<false>(to + first * 2, count, a);
-          write8<false>(to + (p.pairs + first) * 2, count, b);
+          write_values<false, W>(to + first * 2, count, a);
+          write_values<false, W>(to + (p.pairs + first) * 2, count, b);
         } else {
-          write8<F32>(to + first * size, count, a);
-          write8<F32>(to + (p.pairs + first) * size, count, b);
+          write_values<F32, W>(to + first * size, count, a);
+          write_values<F32, W>(to + (p.pairs + first) * size, count, b);
+        }
+      }
+    }
+    __syncthreads();             // (the next tile's table)
+  }
+}
+
+// The same where every unit is whole (the pairs, the values past them and a head are multiples of 16 bytes): no
+// branches between units, so a lane requests several before the table is made.  A unit is 16 bytes
+// (INTERLEAVED) or two times 16: of both halves, or neighbours among the values that are copied (the last ones
+// twice where they are odd).  CACHE: keys and values too.
+template <bool F32, bool INTERLEAVED, bool CACHE>
+__global__ __launch_bounds__(kThreads) void rotate_wide_kernel(RotateArgs p, Units u) {
+  __shared__ float2 table[kTableSize];
+  __shared__ int64_t pages[kMaxRows];
+  __shared__ int32_t places[kMaxRows];
+  constexpr int W = kWide<F32>, PARTS = INTERLEAVED ? 1 : 2, AHEAD = 4 / PARTS;
+  constexpr int64_t size = F32 ? 4 : 2;
+  const int t = threadIdx.x, per_head = u.turned + u.copied, of_k = p.cache.heads * per_head;
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * u.rows; r0 < p.n; r0 += static_cast<int64_t>(gridDim.x) * u.rows) {
+    const int rows = static_cast<int>(min(p.n - r0, static_cast<int64_t>(u.rows))), total = rows * u.of_row;
+    for (int i0 = 0; i0 < total; i0 += AHEAD * kThreads) {
+      int row[AHEAD], head[AHEAD], unit[AHEAD], kind[AHEAD], at[AHEAD][PARTS];     // kind 0: q, 1: k, 2: v
+      uint4 raw[AHEAD][PARTS];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int i = i0 + j * kThreads + t;
+        if (i >= total) continue;
+        const int r = u.row(i);
+        int w = i - r * u.of_row, k = 0;
+        if (CACHE && w >= u.of_q) {
+          w -= u.of_q;
+          k = w >= of_k ? 2 : 1;
+          if (k == 2) w -= of_k;
+        }
+        const int h = CACHE && k == 2 ? u.v_head(w) : u.head(w);
+        w -= h * (CACHE && k == 2 ? u.plain : per_head);
+        const bool turned = w < u.turned && !(CACHE && k == 2);
+        const int past = CACHE && k == 2 ? w : w - u.turned, begin = CACHE && k == 2 ? 0 : 2 * p.pairs;
+        at[j][0] = turned ? w * W : begin + past * W * PARTS;
+        if constexpr (PARTS == 2) at[j][1] = turned ? w * W + p.pairs : min(at[j][0] + W, p.dim - W);
+        row[j] = r, head[j] = h, unit[j] = turned ? w : -1, kind[j] = k;
+        const char* from = static_cast<const char*>(!CACHE || k == 0 ? p.q : k == 1 ? p.k : p.v);
+        from += ((r0 + r) * (!CACHE || k == 0 ? p.ldq : k == 1 ? p.ldk : p.ldv) + static_cast<int64_t>(h) * p.dim) * size;
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) raw[j][q] = load16(from + at[j][q] * size);
+      }
+      if (i0 == 0) {
+        for (int r = t; r < rows; r += kThreads) {
+          const int32_t place = p.positions[r0 + r];
+          places[r] = place;
+          if (CACHE) pages[r] = page_of(p.cache, p.sequence ? p.sequence[r0 + r] : r0 + r, place);
+        }
+        make_table(p, u, r0, rows, table);
+        lds_barrier();                   // (the requests go on)
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        if (i0 + j * kThreads + t >= total) continue;
+        float f[PARTS][W];
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+          const uint32_t e[4] = {raw[j][q].x, raw[j][q].y, raw[j][q].z, raw[j][q].w};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            if constexpr (F32) {
+              f[q][x] = __uint_as_float(e[x]);
+            } else {
+              f[q][2 * x] = __uint_as_float(e[x] << 16);
+              f[q][2 * x + 1] = __uint_as_float(e[x] & 0xffff0000u);
+            }
+          }
+        }
+        const bool turned = unit[j] >= 0;
+        const float2* cs = table + row[j] * p.pairs + (turned ? unit[j] : 0) * (INTERLEAVED ? W / 2 : W);
+        if (turned) {
+          if constexpr (INTERLEAVED) {
+#pragma unroll
+            for (int x = 0; x < W; x += 2) {
+              const float2 c = cs[x / 2];
+              const float y = f[0][x] * c.x - f[0][x + 1] * c.y;
+              f[0][x + 1] = f[0][x + 1] * c.x + f[0][x] * c.y;
+              f[0][x] = y;
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < W; ++x) {
+              const float2 c = cs[x];
+              const float y = f[0][x] * c.x - f[1][x] * c.y;
+              f[1][x] = f[1][x] * c.x + f[0][x] * c.y;
+              f[0][x] = y;
+            }
+          }
+        }
+        const int r = row[j];
+        if (!CACHE || kind[j] == 0) {
+          char* to = static_cast<char*>(p.q_out) + ((r0 + r) * p.ldo + static_cast<int64_t>(head[j]) * p.dim) * size;
+          const bool none = CACHE && p.padding && places[r] < 0;
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) {
+            if (none)
+#pragma unroll
+              for (int x = 0; x < W; ++x) f[q][x] = 0.f;
+            write_values<F32, W>(to + at[j][q] * size, W, f[q]);
+          }
+        } else if (pages[r] >= 0) {
+          uint16_t* to = (kind[j] == 2 ? p.cache.values : p.cache.keys) +
+                         token_at(p.cache, pages[r], head[j], places[r] & ((1 << p.cache.page_shift) - 1));
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) write_values<false, W>(to + at[j][q], W, f[q]);
         }
       }
     }
@@ -201,17 +317,45 @@ constexpr int64_t kMaxGrid = 1 << 16;
 
 }  // namespace
 
+namespace {
+
+template <bool F32, bool INTERLEAVED>
+void launch_wide(const RotateArgs& a, const Units& u, dim3 grid, hipStream_t stream) {
+  if (a.k)
+    hipLaunchKernelGGL((rotate_wide_kernel<F32, INTERLEAVED, true>), grid, dim3(kThreads), 0, stream, a, u);
+  else
+    hipLaunchKernelGGL((rotate_wide_kernel<F32, INTERLEAVED, false>), grid, dim3(kThreads), 0, stream, a, u);
+}
+
+}  // namespace
+
 void decode_rotate(const RotateArgs& a, hipStream_t stream) {
-  const int turned = a.interleaved ? (2 * a.pairs + 7) / 8 : (a.pairs + 7) / 8, copied = (a.dim - 2 * a.pairs + 7) / 8;
-  const int plain = (a.dim + 7) / 8, q_heads = a.q ? a.q_heads : 0, heads = a.k ? a.cache.heads : 0;
+  const int wide = a.f32 ? kWide<true> : kWide<false>, rest = a.dim - 2 * a.pairs;
+  const bool whole = (a.interleaved ? 2 * a.pairs : a.pairs) % wide == 0 && rest % wide == 0 && a.dim % wide == 0;
+  // (a whole unit of halves is two vectors)
+  const int vectors = whole && !a.interleaved ? 2 : 1;
+  auto units = [&](int values, int of) { return (values + wide * of - 1) / (wide * of); };
+  const int turned = units(a.interleaved ? 2 * a.pairs : a.pairs, 1), copied = units(rest, vectors);
+  const int plain = units(a.dim, vectors), q_heads = a.q ? a.q_heads : 0, heads = a.k ? a.cache.heads : 0;
   const int of_q = q_heads * (turned + copied), of_row = of_q + heads * (turned + copied + plain);
-  // Tiles of about 1024 units (4 a lane), fewer where the rows would not fill the CUs.
-  int64_t rows = 1024 / of_row;
+  // Rows of a tile, fewer where they would not fill the CUs: about two units per lane (16383 rows of 20 heads of 96 in float32:
+  // 41 us with a row of 480 units each, 44 to 50 with 2 to 8), and with a cache more, for each tile waits for its
+  // rows' pages (6000 rows of 48 heads of 128 in bf16: 31 us with a row of 384 units each, 26 with 6 or 8).
+  int64_t rows = (whole ? a.k ? 3072 : 512 : 1024) / of_row;
   if (a.pairs) rows = std::min<int64_t>(rows, kTableSize / a.pairs);
-  rows = std::max<int64_t>(1, std::min<int64_t>({rows, kMaxRows, a.n / 1024}));
-  const Units u{static_cast<int>(rows), turned, copied, plain, of_q, of_row, Divide(of_row), Divide(turned + copied), Divide(plain)};
+  rows = std::max<int64_t>(1, std::min<int64_t>({rows, kMaxRows, a.n / (a.k ? 512 : 1024)}));
+  const Units u{static_cast<int>(rows), turned, copied, plain, of_q, of_row, Divide(of_row), Divide(turned + copied), Divide(plain),
+                Divide(std::max(1, a.pairs))};
   const dim3 grid(static_cast<unsigned>(std::min((a.n + rows - 1) / rows, kMaxGrid)));
-  if (a.f32)
+  if (whole && a.f32 && a.interleaved)
+    launch_wide<true, true>(a, u, grid, stream);
+  else if (whole && a.f32)
+    launch_wide<true, false>(a, u, grid, stream);
+  else if (whole && a.interleaved)
+    launch_wide<false, true>(a, u, grid, stream);
+  else if (whole)
+    launch_wide<false, false>(a, u, grid, stream);
+  else if (a.f32)
     hipLaunchKernelGGL(rotate_kernel<true>, grid, dim3(kThreads), 0, stream, a, u);
   else
     hipLaunchKernelGGL(rotate_kernel<false>, grid, dim3(kThreads), 0, stream, a, u);
