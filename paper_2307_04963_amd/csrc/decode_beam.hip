@@ -85,7 +85,7 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
 }
 
 struct Segments {
-  int count;                           // of a row
+  int count, size;                     // of a row; words of one
   float2* state;                       // [row][segment]: maximum, sum of exponentials around it
   uint64_t* lists;                     // [row][segment][k] keys, largest first, 0 past the last
 };
@@ -142,15 +142,32 @@ __global__ __launch_bounds__(kThreads) void segment_kernel(BeamArgs p, Segments 
   // beams without candidates of their own: the second kernel skips them too
   const float score = p.scores[row];
   if ((p.ended && p.ended[row]) || !(score > kClosed)) return;     // (the same for the whole workgroup)
+  float tops[2 * V], top, m, sum = 0.f;                // of four values, of all the lane's, of the wave's
+  auto maxima = [&] {
 #pragma unroll
-  for (int i = 0; i < 8 * V; ++i) v[i] = fminf(fmaxf(v[i], kClosed), kLargest);     // NaN is closed, +infinity the largest finite value
-  float top = v[0];
+    for (int i = 0; i < 2 * V; ++i) tops[i] = fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3]));
+    top = tops[0];
 #pragma unroll
-  for (int i = 1; i < 8 * V; ++i) top = fmaxf(top, v[i]);
-  const float m = wave_top(top), around = m == kClosed ? 0.f : m;
-  float sum = 0.f;
+    for (int i = 1; i < 2 * V; ++i) top = fmaxf(top, tops[i]);
+    m = wave_top(top);
+  };
+  maxima();
+  // Ordinary values: 2^(v log2 e - a) by one multiplication and addition, a the rounded m log2 e, and what that
+  // rounding took put right at the end.
+  const float a = m == kClosed ? 0.f : m * kLog2e;
 #pragma unroll
-  for (int i = 0; i < 8 * V; ++i) sum += __builtin_amdgcn_exp2f((v[i] - around) * kLog2e);
+  for (int i = 0; i < 8 * V; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i], kLog2e, -a));
+  if (m != kClosed) sum *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, kLog2e, -a));
+  if (__any(!(sum < kLargest)) || (m != kClosed && !(fabsf(m) < 1e30f))) {
+    // NaN among them, which is closed, +infinity, which is the largest finite value, or a product beyond it
+#pragma unroll
+    for (int i = 0; i < 8 * V; ++i) v[i] = fminf(fmaxf(v[i], kClosed), kLargest);
+    maxima();
+    const float around = m == kClosed ? 0.f : m;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8 * V; ++i) sum += __builtin_amdgcn_exp2f((v[i] - around) * kLog2e);
+  }
   sum = wave_sum(sum);
   if (lane == 0) waves[wave] = make_float2(m, sum);
   const float bound = bound_of_all(s, top, p.k);
@@ -161,14 +178,14 @@ __global__ __launch_bounds__(kThreads) void segment_kernel(BeamArgs p, Segments 
     for (int w = 0; w < kWaves; ++w) total += __builtin_amdgcn_exp2f((waves[w].x - base2) * kLog2e) * waves[w].y;
     g.state[item] = make_float2(all, total);
   }
-  if (__any(top >= bound)) {
 #pragma unroll
-    for (int i = 0; i < 8 * V; ++i)
-      if (__any(v[i] >= bound)) {                      // (few: most are one comparison for the wave)
-        if (v[i] >= bound && v[i] > kClosed) {
-          const int at = atomicAdd(&s.count, 1);
-          if (at < kRoom) s.keys[at] = key_of(v[i], index(i));
-        }
+  for (int i = 0; i < 2 * V; ++i) {
+    if (!__any(tops[i] >= bound)) continue;            // (few: most are one comparison for four values of 64 lanes)
+#pragma unroll
+    for (int j = 4 * i; j < 4 * i + 4; ++j)
+      if (v[j] >= bound && v[j] > kClosed) {
+        const int at = atomicAdd(&s.count, 1);
+        if (at < kRoom) s.keys[at] = key_of(v[j], index(j));
       }
   }
   __syncthreads();
@@ -197,8 +214,9 @@ __global__ __launch_bounds__(kThreads) void segment_kernel(BeamArgs p, Segments 
 }
 
 // One sequence: its beams' sums, then the k largest of all lists.  FLAT: a thread keeps up to kFlat of the lists' entries,
-// requested at once; else it walks along the lists.
-constexpr int kFlat = 8;
+// requested at once.  Else the k lists with the largest first entries are chosen (any other's first entry has k
+// larger ones), and their entries, k * k at most, kept.
+constexpr int kFlat = 8, kKept = kBeamMaxK * kBeamMaxK / kThreads;
 template <bool FLAT>
 __global__ __launch_bounds__(kThreads) void choose_kernel(BeamArgs p, Segments g) {
   __shared__ Chosen s;
@@ -208,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(BeamArgs p, Segments g
   const int64_t b = blockIdx.x;
   const int lists = p.beams * g.count, entries = lists * p.k;
   const uint64_t* all = g.lists + b * entries;
-  uint64_t own[FLAT ? kFlat : 1];
+  uint64_t own[FLAT ? kFlat : kKept];
   if constexpr (FLAT) {
     // The lists' first entries first, so that every wave has some of them.  (Of a beam without candidates the entries are
     // whatever the workspace held; they are not used.)
@@ -257,44 +275,78 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(BeamArgs p, Segments g
     if (!key || shift[w].x == kClosed) return 0;
     return key_of((value_of(static_cast<uint32_t>(key >> 32)) - shift[w].x) + shift[w].y, w * p.words + index_of(key));
   };
-  auto key_at = [&](int list, int i) {           // (a list of a closed beam is not read)
-    const int w = list / g.count;
-    return shift[w].x == kClosed ? uint64_t(0) : valued(all[static_cast<int64_t>(list) * p.k + i], w);
+  const uint64_t ended = threadIdx.x < p.beams && kept[threadIdx.x] > kClosed ? key_of(kept[threadIdx.x], threadIdx.x * p.words + p.end) : 0;
+  auto value_at = [](uint64_t key) { return key ? value_of(static_cast<uint32_t>(key >> 32)) : kClosed; };
+  // keys that reach the bound, into LDS; visible after it
+  auto take = [&](uint64_t key, float bound) {
+    if (!key || value_at(key) < bound) return;
+    const int at = atomicAdd(&s.count, 1);
+    if (at < kRoom) s.keys[at] = key;
   };
-  uint64_t head = 0;
+  // the largest of the workgroup's best(before), those of each thread below `before`
+  auto next = [&](uint64_t best) {
+    best = wave_max(best);
+    if (lane == 0) s.best[wave] = best;
+    __syncthreads();
+    best = max(max(s.best[0], s.best[1]), max(s.best[2], s.best[3]));
+    __syncthreads();
+    return best;
+  };
   if constexpr (FLAT) {
 #pragma unroll
     for (int j = 0; j < kFlat; ++j) {
       const int i = threadIdx.x + j * kThreads;
       if (j * kThreads < entries && i < entries) own[j] = valued(own[j], i % lists / g.count);
-      head = max(head, own[j]);
     }
   } else {
+    __shared__ int chosen[kBeamMaxK];
+    auto key_at = [&](int list, int i) {         // (a list of a closed beam is not read)
+      const int w = list / g.count;
+      return shift[w].x == kClosed ? uint64_t(0) : valued(all[static_cast<int64_t>(list) * p.k + i], w);
+    };
+    auto list_of = [&](uint64_t key) {
+      const int w = static_cast<int>(index_of(key) / p.words);
+      return w * g.count + static_cast<int>(index_of(key) - w * p.words) / g.size;
+    };
+    if (threadIdx.x < p.k) chosen[threadIdx.x] = -1;
+    uint64_t head = 0;
     for (int i = threadIdx.x; i < lists; i += kThreads) head = max(head, key_at(i, 0));
-  }
-  const uint64_t ended = threadIdx.x < p.beams && kept[threadIdx.x] > kClosed ? key_of(kept[threadIdx.x], threadIdx.x * p.words + p.end) : 0;
-  head = max(head, ended);
-  const float bound = bound_of_all(s, head ? value_of(static_cast<uint32_t>(head >> 32)) : kClosed, p.k);
-  auto reaches = [&](uint64_t key) { return key && !(value_of(static_cast<uint32_t>(key >> 32)) < bound); };
-  auto each = [&](auto&& f) {                      // the thread's candidates that reach the bound
-    if constexpr (FLAT) {
-#pragma unroll
-      for (int j = 0; j < kFlat; ++j)
-        if (reaches(own[j])) f(own[j]);
+    const float bound = bound_of_all(s, value_at(head), p.k);
+    for (int i = threadIdx.x; i < lists; i += kThreads) take(key_at(i, 0), bound);
+    __syncthreads();
+    if (s.count <= kRoom) {
+      rank_all(s, p.k, [&](int rank, uint64_t key) { chosen[rank] = list_of(key); });
     } else {
-      for (int i = threadIdx.x; i < lists; i += kThreads)
-        for (int j = 0; j < p.k; ++j) {
-          const uint64_t key = key_at(i, j);
-          if (!reaches(key)) break;
-          f(key);
+      uint64_t before = ~uint64_t(0);
+      for (int round = 0; round < p.k; ++round) {
+        uint64_t best = 0;
+        for (int i = threadIdx.x; i < lists; i += kThreads) {
+          const uint64_t key = key_at(i, 0);
+          best = key < before && key > best ? key : best;
         }
+        before = next(best);
+        if (threadIdx.x == 0 && before) chosen[round] = list_of(before);
+      }
     }
-    if (ended) f(ended);
-  };
-  each([&](uint64_t key) {
-    const int at = atomicAdd(&s.count, 1);
-    if (at < kRoom) s.keys[at] = key;
-  });
+    __syncthreads();
+    if (threadIdx.x == 0) s.count = 0;
+#pragma unroll
+    for (int j = 0; j < kKept; ++j) {
+      const int i = threadIdx.x + j * kThreads;
+      own[j] = 0;
+      if (j * kThreads < p.k * p.k && i < p.k * p.k) {
+        const int list = chosen[i % p.k];        // (first entries first, as above)
+        if (list >= 0) own[j] = key_at(list, i / p.k);
+      }
+    }
+  }
+  uint64_t head = ended;
+#pragma unroll
+  for (uint64_t key : own) head = max(head, key);
+  const float bound = bound_of_all(s, value_at(head), p.k);
+#pragma unroll
+  for (uint64_t key : own) take(key, bound);
+  take(ended, bound);
   __syncthreads();
   auto put = [&](int rank, uint64_t key) {
     const int64_t at = b * p.k + rank;
@@ -318,15 +370,11 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(BeamArgs p, Segments g
   }
   uint64_t before = ~uint64_t(0);
   for (int round = 0; round < p.k; ++round) {
-    uint64_t best = 0;
-    each([&](uint64_t key) { best = key < before && key > best ? key : best; });
-    best = wave_max(best);
-    if (lane == 0) s.best[wave] = best;
-    __syncthreads();
-    best = max(max(s.best[0], s.best[1]), max(s.best[2], s.best[3]));
-    if (threadIdx.x == 0) put(round, best);
-    before = best;
-    __syncthreads();
+    uint64_t best = ended < before ? ended : 0;
+#pragma unroll
+    for (uint64_t key : own) best = key < before && key > best ? key : best;
+    before = next(best);
+    if (threadIdx.x == 0) put(round, before);
   }
 }
 
@@ -354,6 +402,7 @@ size_t decode_beam_workspace(int64_t sequences, int beams, int words, int k) {
 void decode_beam(const BeamArgs& a, hipStream_t stream) {
   Segments g;
   g.count = segments_of(a.words);
+  g.size = kThreads * 8 * groups_of(a.words);
   const uint32_t items = static_cast<uint32_t>(a.sequences * a.beams * g.count);     // (below 2^24 rows of at most 128)
   g.lists = static_cast<uint64_t*>(a.workspace);
   g.state = reinterpret_cast<float2*>(g.lists + static_cast<int64_t>(items) * a.k);

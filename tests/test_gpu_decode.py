@@ -419,6 +419,23 @@ def test_beam_widths(de, beams, k):
     check_beam(de, 2, beams, 9001, k, F, first=True)
 
 
+@pytest.mark.parametrize("beams, words, k", [(16, 200000, 32), (64, 70000, 64), (9, 131072, 64), (64, 262144, 3), (33, 5000, 64), (2, 1 << 20, 64)])
+def test_beam_many_lists(de, beams, words, k):
+    """More lists of candidates than a workgroup keeps at once."""
+    check_beam(de, 1, beams, words, k, F)
+    check_beam(de, 2, beams, words, k, F, ended=0.3, closed=0.05, spread=1.0)
+
+
+def test_beam_many_equal_lists(de):
+    for beams, words, k in ((64, 70000, 64), (40, 200000, 5)):
+        got = de.beam(torch.zeros((beams, words), dtype=B, device="cuda"), torch.zeros(beams, device="cuda"), beams, k=k)
+        assert got.parents[0].tolist() == [0] * k and got.tokens[0].tolist() == list(range(k))
+        z = torch.zeros((beams, words), device="cuda")
+        z[:, 7] = -1.0                                      # (every beam's words weigh the same)
+        got = de.beam(z, torch.arange(beams, device="cuda") * 0.5, beams, k=k)
+        assert got.parents[0].tolist() == [beams - 1] * k and got.tokens[0].tolist() == [i for i in range(k + 1) if i != 7][:k]
+
+
 def test_beam_many_sequences(de):
     check_beam(de, 200, 2, 501, 2, F, ended=0.2)
     check_beam(de, 33, 4, 12345, 4, F)
