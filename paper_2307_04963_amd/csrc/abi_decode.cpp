@@ -108,7 +108,7 @@ int dycl_op_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const
     need(!q || (q_heads >= 1 && int64_t(q_heads) * dim <= kRotateMaxWidth), op, "q_heads below 1 or q_heads * dim above 65536");
     need(sequence || n == sequences, op, "without `sequence` there are as many rows as sequences");
     if (n == 0) return static_cast<int>(DYCL_OK);
-    need(k && v && positions && tables && keys && values, op, "null k, v, positions, tables, keys or values");
+    need(k && v && positions && (tables || sequences == 0) && keys && values, op, "null k, v, positions, tables, keys or values");
     const int64_t width = int64_t(heads) * dim, q_width = int64_t(q_heads) * dim;
     need(pitch_ok(ldk, width) && pitch_ok(ldv, width) && (!q || (pitch_ok(ldq, q_width) && pitch_ok(ldo, q_width))) &&
              pitch_ok(ldt, max_pages),
@@ -169,7 +169,7 @@ int dycl_op_attend(const uint16_t* q, int64_t ldq, int64_t n, int q_heads, int h
     need(scale - scale == 0.f, op, "scale not finite");
     need(sequence || n == sequences, op, "without `sequence` there are as many rows as sequences");
     if (n == 0) return static_cast<int>(DYCL_OK);
-    need(q && keys && values && tables && lengths && out, op, "null q, keys, values, tables, lengths or out");
+    need(q && keys && values && (tables || sequences == 0) && lengths && out, op, "null q, keys, values, tables, lengths or out");
     const int64_t width = int64_t(q_heads) * dim;
     need(pitch_ok(ldq, width) && pitch_ok(ldo, width) && pitch_ok(ldt, max_pages) && (!mask || pitch_ok(ldm, max_length)), op,
          "a row pitch below the row");
@@ -258,7 +258,7 @@ int dycl_op_fork(const int32_t* tables, int64_t ldt, const int32_t* lengths, int
     need_sizes(op, keys ? heads : 1, page, keys ? dim : 8, max_pages, keys ? pages : 1, rows);
     if (n == 0) return static_cast<int>(DYCL_OK);
     need(keys || new_tables, op, "neither a cache nor new tables");
-    need(tables && lengths && parents && fresh, op, "null tables, lengths, parents or fresh");
+    need(((tables && lengths) || rows == 0) && parents && fresh, op, "null tables, lengths, parents or fresh");
     need(pitch_ok(ldt, max_pages) && (!new_tables || pitch_ok(ldn, max_pages)), op, "a row pitch below the row");
     need(at(tables, 4) && at(lengths, 4) && at(parents, 4) && at(fresh, 4) && at(new_tables, 4) && at(new_lengths, 4) &&
              at(keys, 16) && at(values, 16),
