@@ -59,6 +59,17 @@ __device__ __forceinline__ void write_values(void* p, int count, const float* f)
   }
 }
 
+// N values, 4 to 16 bytes of them, to any element
+template <bool F32, int N>
+__device__ __forceinline__ void put_values(void* p, const float* f) {
+  constexpr int WORDS = F32 ? N : N / 2;
+  typedef uint32_t words __attribute__((ext_vector_type(WORDS), aligned(2)));
+  words w;
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i) w[i] = F32 ? __float_as_uint(f[i]) : pack_bf16(f[F32 ? i : 2 * i], f[F32 ? i : 2 * i + 1]);
+  *static_cast<words*>(p) = w;
+}
+
 // the page of place `at` of a sequence's table, or -1
 __device__ __forceinline__ int64_t page_of(const PagedArgs& c, int64_t sequence, int64_t at) {
   if (sequence < 0 || sequence >= c.sequences || at < 0) return -1;

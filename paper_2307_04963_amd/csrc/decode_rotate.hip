@@ -6,8 +6,9 @@
 // it is reduced to an eighth of a turn around the nearest quarter; sine and cosine of
 // that are Taylor polynomials in float32 (remainders below 2^-28 at pi / 4).
 //
-// Bound by HBM: every value is read and written once (measured: 251 MB of float32 41 us, 6.1 TB/s; prompts of 6000
-// rows into the cache, 157 MB, 26 us; one token of 32 heads 2.2 us, a launch).  A workgroup takes a tile of rows;
+// Bound by HBM: every value is read and written once (measured: 251 MB of float32 39 us, 6.4 TB/s; prompts of 6000
+// rows into the cache, 157 MB, 26 us; one token of 32 heads 2.0 us, a launch; units of 8 or 4 bytes 4 to 5.5 TB/s,
+// odd ones 1.7 in bf16).  A workgroup takes a tile of rows;
 // their cosines and sines are made once into LDS for all of a row's heads, then a lane
 // takes 16 bytes (of each half, or of neighbours), at any alignment.
 #include "decode_dev.hpp"
@@ -173,27 +174,27 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs p, Units u)
   }
 }
 
-// The same where every unit is whole (the pairs, the values past them and a head are multiples of 16 bytes): no
-// branches between units, so a lane requests several before the table is made.  A unit is 16 bytes
-// (INTERLEAVED) or two times 16: of both halves, or neighbours among the values that are copied (the last ones
+// The same where every unit is whole (the pairs, the values past them and a head are multiples of W values): no
+// branches between units, so a lane requests several before the table is made.  A unit is W values
+// (INTERLEAVED) or two times W: of both halves, or neighbours among the values that are copied (the last ones
 // twice where they are odd).  CACHE: keys and values too.
-template <bool F32, bool INTERLEAVED, bool CACHE>
+template <bool F32, int W, bool INTERLEAVED, bool CACHE>
 __global__ __launch_bounds__(kThreads) void rotate_wide_kernel(RotateArgs p, Units u) {
   __shared__ float2 table[kTableSize];
   __shared__ int64_t pages[kMaxRows];
   __shared__ int32_t places[kMaxRows];
-  constexpr int W = kWide<F32>, PARTS = INTERLEAVED ? 1 : 2, AHEAD = 4 / PARTS;
+  constexpr int PARTS = INTERLEAVED ? 1 : 2, WORDS = F32 ? W : W / 2, AHEAD = (WORDS == 4 ? 4 : 8) / PARTS;
   constexpr int64_t size = F32 ? 4 : 2;
+  typedef uint32_t words __attribute__((ext_vector_type(WORDS), aligned(2)));
   const int t = threadIdx.x, per_head = u.turned + u.copied, of_k = p.cache.heads * per_head;
   for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * u.rows; r0 < p.n; r0 += static_cast<int64_t>(gridDim.x) * u.rows) {
     const int rows = static_cast<int>(min(p.n - r0, static_cast<int64_t>(u.rows))), total = rows * u.of_row;
     for (int i0 = 0; i0 < total; i0 += AHEAD * kThreads) {
       int row[AHEAD], head[AHEAD], unit[AHEAD], kind[AHEAD], at[AHEAD][PARTS];     // kind 0: q, 1: k, 2: v
-      uint4 raw[AHEAD][PARTS];
+      words raw[AHEAD][PARTS];
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j) {
-        const int i = i0 + j * kThreads + t;
-        if (i >= total) continue;
+        const int i = min(i0 + j * kThreads + t, total - 1);     // (past the end the last one again: no branch here either)
         const int r = u.row(i);
         int w = i - r * u.of_row, k = 0;
         if (CACHE && w >= u.of_q) {
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void rotate_wide_kernel(RotateArgs p, Uni
         const char* from = static_cast<const char*>(!CACHE || k == 0 ? p.q : k == 1 ? p.k : p.v);
         from += ((r0 + r) * (!CACHE || k == 0 ? p.ldq : k == 1 ? p.ldk : p.ldv) + static_cast<int64_t>(h) * p.dim) * size;
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) raw[j][q] = load16(from + at[j][q] * size);
+        for (int q = 0; q < PARTS; ++q) raw[j][q] = *reinterpret_cast<const words*>(from + at[j][q] * size);
       }
       if (i0 == 0) {
         for (int r = t; r < rows; r += kThreads) {
@@ -228,14 +229,14 @@ __global__ __launch_bounds__(kThreads) void rotate_wide_kernel(RotateArgs p, Uni
         float f[PARTS][W];
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {
-          const uint32_t e[4] = {raw[j][q].x, raw[j][q].y, raw[j][q].z, raw[j][q].w};
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
+          for (int x = 0; x < WORDS; ++x) {
+            const uint32_t e = raw[j][q][x];
             if constexpr (F32) {
-              f[q][x] = __uint_as_float(e[x]);
+              f[q][x] = __uint_as_float(e);
             } else {
-              f[q][2 * x] = __uint_as_float(e[x] << 16);
-              f[q][2 * x + 1] = __uint_as_float(e[x] & 0xffff0000u);
+              f[q][2 * x] = __uint_as_float(e << 16);
+              f[q][2 * x + 1] = __uint_as_float(e & 0xffff0000u);
             }
           }
         }
@@ -269,13 +270,13 @@ __global__ __launch_bounds__(kThreads) void rotate_wide_kernel(RotateArgs p, Uni
             if (none)
 #pragma unroll
               for (int x = 0; x < W; ++x) f[q][x] = 0.f;
-            write_values<F32, W>(to + at[j][q] * size, W, f[q]);
+            put_values<F32, W>(to + at[j][q] * size, f[q]);
           }
         } else if (pages[r] >= 0) {
           uint16_t* to = (kind[j] == 2 ? p.cache.values : p.cache.keys) +
                          token_at(p.cache, pages[r], head[j], places[r] & ((1 << p.cache.page_shift) - 1));
 #pragma unroll
-          for (int q = 0; q < PARTS; ++q) write_values<false, W>(to + at[j][q], W, f[q]);
+          for (int q = 0; q < PARTS; ++q) put_values<false, W>(to + at[j][q], f[q]);
         }
       }
     }
@@ -319,19 +320,28 @@ constexpr int64_t kMaxGrid = 1 << 16;
 
 namespace {
 
-template <bool F32, bool INTERLEAVED>
+template <bool F32, int W>
 void launch_wide(const RotateArgs& a, const Units& u, dim3 grid, hipStream_t stream) {
-  if (a.k)
-    hipLaunchKernelGGL((rotate_wide_kernel<F32, INTERLEAVED, true>), grid, dim3(kThreads), 0, stream, a, u);
+  if (a.k && a.interleaved)
+    hipLaunchKernelGGL((rotate_wide_kernel<F32, W, true, true>), grid, dim3(kThreads), 0, stream, a, u);
+  else if (a.k)
+    hipLaunchKernelGGL((rotate_wide_kernel<F32, W, false, true>), grid, dim3(kThreads), 0, stream, a, u);
+  else if (a.interleaved)
+    hipLaunchKernelGGL((rotate_wide_kernel<F32, W, true, false>), grid, dim3(kThreads), 0, stream, a, u);
   else
-    hipLaunchKernelGGL((rotate_wide_kernel<F32, INTERLEAVED, false>), grid, dim3(kThreads), 0, stream, a, u);
+    hipLaunchKernelGGL((rotate_wide_kernel<F32, W, false, false>), grid, dim3(kThreads), 0, stream, a, u);
 }
 
 }  // namespace
 
 void decode_rotate(const RotateArgs& a, hipStream_t stream) {
-  const int wide = a.f32 ? kWide<true> : kWide<false>, rest = a.dim - 2 * a.pairs;
-  const bool whole = (a.interleaved ? 2 * a.pairs : a.pairs) % wide == 0 && rest % wide == 0 && a.dim % wide == 0;
+  // Values of a unit: 16, 8 or 4 bytes, the most that the sizes are multiples of.  (Pairs of which no two lie together in float32,
+  // or four in bf16: the kernel that looks at every unit's length, at a third of the rate.)
+  const int rest = a.dim - 2 * a.pairs, most = a.f32 ? kWide<true> : kWide<false>;
+  int wide = most;
+  while (wide > 1 && ((a.interleaved ? 2 * a.pairs : a.pairs) % wide || rest % wide || a.dim % wide)) wide /= 2;
+  const bool whole = wide > 1;
+  if (!whole) wide = most;
   // (a whole unit of halves is two vectors)
   const int vectors = whole && !a.interleaved ? 2 : 1;
   auto units = [&](int values, int of) { return (values + wide * of - 1) / (wide * of); };
@@ -341,20 +351,22 @@ void decode_rotate(const RotateArgs& a, hipStream_t stream) {
   // Rows of a tile, fewer where they would not fill the CUs: about two units per lane (16383 rows of 20 heads of 96 in float32:
   // 41 us with a row of 480 units each, 44 to 50 with 2 to 8), and with a cache more, for each tile waits for its
   // rows' pages (6000 rows of 48 heads of 128 in bf16: 31 us with a row of 384 units each, 26 with 6 or 8).
-  int64_t rows = (whole ? a.k ? 3072 : 512 : 1024) / of_row;
+  int64_t rows = (whole ? (a.k ? 3072 : 512) * (most / wide) : 1024) / of_row;
   if (a.pairs) rows = std::min<int64_t>(rows, kTableSize / a.pairs);
   rows = std::max<int64_t>(1, std::min<int64_t>({rows, kMaxRows, a.n / (a.k ? 512 : 1024)}));
   const Units u{static_cast<int>(rows), turned, copied, plain, of_q, of_row, Divide(of_row), Divide(turned + copied), Divide(plain),
                 Divide(std::max(1, a.pairs))};
   const dim3 grid(static_cast<unsigned>(std::min((a.n + rows - 1) / rows, kMaxGrid)));
-  if (whole && a.f32 && a.interleaved)
-    launch_wide<true, true>(a, u, grid, stream);
-  else if (whole && a.f32)
-    launch_wide<true, false>(a, u, grid, stream);
-  else if (whole && a.interleaved)
-    launch_wide<false, true>(a, u, grid, stream);
+  if (a.f32 && wide == 4 && whole)
+    launch_wide<true, 4>(a, u, grid, stream);
+  else if (a.f32 && whole)
+    launch_wide<true, 2>(a, u, grid, stream);
+  else if (whole && wide == 8)
+    launch_wide<false, 8>(a, u, grid, stream);
+  else if (whole && wide == 4)
+    launch_wide<false, 4>(a, u, grid, stream);
   else if (whole)
-    launch_wide<false, false>(a, u, grid, stream);
+    launch_wide<false, 2>(a, u, grid, stream);
   else if (a.f32)
     hipLaunchKernelGGL(rotate_kernel<true>, grid, dim3(kThreads), 0, stream, a, u);
   else
