@@ -227,6 +227,7 @@ def test_attend_dims_and_pages(de, dim, page):
 
 @pytest.mark.parametrize("q_heads, heads", [(1, 1), (3, 3), (16, 16), (5, 1), (32, 8), (16, 1), (17, 1), (40, 1), (64, 2), (128, 1)])
 def test_attend_heads(de, q_heads, heads):
+    check_attend(de, [100, 0, 700], q_heads, heads, 256, 16)
     check_attend(de, [0, 1, 33, 150], q_heads, heads, 64, 16)
     check_attend(de, [300, 1, 33, 900], q_heads, heads, 128, 32, holes=0.2, pad=3)
 
@@ -329,7 +330,8 @@ def test_attend_infinite_values(de):
 
 @pytest.mark.parametrize("n, heads, q_heads, dim, most, page, window", [
     (40, 2, 8, 128, 100, 16, 0), (40, 2, 8, 128, 5000, 64, 0), (400, 1, 2, 64, 5000, 64, 0), (700, 2, 2, 64, 700, 8, 0), (90, 4, 20, 256, 7000, 32, 0),
-    (300, 2, 2, 72, 4500, 128, 4200), (48, 8, 8, 64, 33000, 256, 0), (64, 2, 66, 128, 9000, 64, 0)])
+    (300, 2, 2, 72, 4500, 128, 4200), (48, 8, 8, 64, 33000, 256, 0), (64, 2, 66, 128, 9000, 64, 0),
+    (64, 1, 32, 256, 9000, 64, 0), (70, 1, 16, 200, 33000, 1024, 0)])
 def test_attend_company_leaves_bits(de, n, heads, q_heads, dim, most, page, window):
     """A row's bits do not depend on the other rows, on the page order or on what is behind its keys."""
     g = gen(15 + n)

@@ -93,3 +93,23 @@ def test_steps_over_beams():
         history = [history[p] for p in b.parents.view(-1).tolist()]
         tokens, scores, ended = b.tokens.view(-1).long(), b.scores.view(-1), b.ended.view(-1)
     assert int(ended.sum()) > 0
+
+
+def test_example():
+    """The example decoder runs, orders its beams, keeps ended ones, and one sequence's beams are the same alone."""
+    from examples import beam_decoder as bd
+    model = bd.build(blocks=2, d=128, f=192, heads=4, kv_heads=2, dim=32, words=97, end=5)
+    lengths, steps = [9, 40, 17], 37
+    states = torch.randn((sum(lengths), 128), device="cuda", generator=gen(2)).bfloat16()
+    first = torch.zeros(3, dtype=torch.int64, device="cuda")
+    said, scores = model(first, model.encode(states, lengths), 4, steps)
+    assert said.shape == (3, 4, steps) and bool(torch.isfinite(scores).all())
+    assert bool((scores[:, :-1] >= scores[:, 1:]).all()) and int(said.min()) >= 0 and int(said.max()) < 97
+    for tokens in said.view(-1, steps).tolist():
+        if 5 in tokens:
+            assert set(tokens[tokens.index(5):]) == {5}
+    for s in range(3):
+        assert len({tuple(t) for t in said[s].tolist()}) == 4
+        at = sum(lengths[:s])
+        alone, alone_scores = model(first[:1], model.encode(states[at:at + lengths[s]], lengths[s:s + 1]), 4, steps)
+        assert torch.equal(alone[0], said[s]) and torch.equal(alone_scores[0], scores[s])
