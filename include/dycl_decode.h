@@ -100,8 +100,8 @@ int dycl_op_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const
  *   window        0 (none) or the number of last places seen.
  *   workspace     dycl_op_attend_workspace(...) bytes, 16-byte aligned, or NULL when that is 0.
  * Scores, softmax and sums are float32.  The softmax's weights enter the second product as
- * two bf16 terms (16 significant bits).  The keys are summed in parts that only
- * max_length, window and the head counts set, joined in order.
+ * two bf16 terms (16 significant bits).  The keys are summed in parts that the
+ * dim alone sets, joined in a fixed order.  -1e38 < scale < 1e38,
  * q_heads a multiple of heads, n * q_heads < 2^31, max_length < 2^31 - 4096.
  */
 size_t dycl_op_attend_workspace(int64_t n, int q_heads, int heads, int dim, int64_t max_length, int64_t window);
@@ -118,7 +118,7 @@ int dycl_op_attend(const uint16_t* q, int64_t ldq, int64_t n, int q_heads, int h
  * the k largest, largest first, the lowest w * words + t among equals.
  * A beam that has ended is one candidate: `end`, with its score as it is.
  * A logit of -infinity or NaN is a closed token, +infinity counts as the
- * largest finite value; a beam whose score is -infinity or NaN has no candidates.
+ * largest finite value, of a score too; a beam whose score is -infinity or NaN has no candidates.
  * An end token outside [0, words) ends no beam (then `ended` must be NULL).
  *   logits     [sequences * beams][words] type, pitch ldl.
  *   scores     [sequences * beams] float32: sums of logarithms so far.

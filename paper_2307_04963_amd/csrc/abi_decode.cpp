@@ -51,6 +51,9 @@ PagedArgs paged(const uint16_t* keys, const uint16_t* values, int64_t pages, int
   return c;
 }
 
+// a window that reaches as far as any row is none
+int64_t window_of(int64_t window, int64_t max_length) { return window >= max_length ? 0 : window; }
+
 const char* const kUnaligned = "a pointer not aligned to its element (keys, values, workspace: 16 bytes)";
 
 }  // namespace
@@ -149,7 +152,7 @@ size_t dycl_op_attend_workspace(int64_t n, int q_heads, int heads, int dim, int6
   if (n < 1 || n >= kMaxRows || heads < 1 || q_heads < heads || q_heads % heads || n * q_heads >= kMaxRows || dim < 8 ||
       dim > kAttendMaxDim || max_length < 0 || max_length >= kMaxRows - 4096 || window < 0)
     return 0;
-  return decode_attend_workspace(n, q_heads, heads, dim, max_length, window);
+  return decode_attend_workspace(n, q_heads, heads, dim, max_length, window_of(window, max_length));
 }
 
 int dycl_op_attend(const uint16_t* q, int64_t ldq, int64_t n, int q_heads, int heads, int dim, float scale,
@@ -166,7 +169,7 @@ int dycl_op_attend(const uint16_t* q, int64_t ldq, int64_t n, int q_heads, int h
     need(max_length >= 0 && max_length <= int64_t(max_pages) * page && max_length < kMaxRows - 4096, op,
          "max_length outside [0, max_pages * page] or above 2^31 - 4097");
     need(window >= 0, op, "negative window");
-    need(scale - scale == 0.f, op, "scale not finite");
+    need(scale > -1e38f && scale < 1e38f, op, "scale not finite, or above 1e38");
     need(sequence || n == sequences, op, "without `sequence` there are as many rows as sequences");
     if (n == 0) return static_cast<int>(DYCL_OK);
     need(q && keys && values && (tables || sequences == 0) && lengths && out, op, "null q, keys, values, tables, lengths or out");
@@ -177,6 +180,7 @@ int dycl_op_attend(const uint16_t* q, int64_t ldq, int64_t n, int q_heads, int h
              at(workspace, 16),
          op, kUnaligned);
     need(out != q, op, "out is q");
+    window = window_of(window, max_length);
     const size_t bytes = decode_attend_workspace(n, q_heads, heads, dim, max_length, window);
     need(bytes == 0 || (workspace && workspace_bytes >= bytes), op, "workspace too small");
     AttendArgs a{};

@@ -79,6 +79,7 @@ def _attend(**kw):
 @pytest.mark.parametrize("bad, word", SIZES + [
     (dict(n=-1), "n outside"), (dict(qh=7), "multiple of heads"), (dict(qh=1), "multiple of heads"), (dict(n=1 << 30, sequences=1 << 30), "n * q_heads"),
     (dict(max_length=129), "max_length"), (dict(max_length=-1), "max_length"), (dict(window=-1), "window"), (dict(scale=float("nan")), "scale"),
+    (dict(scale=float("inf")), "scale"), (dict(scale=-2e38), "scale"),
     (dict(n=3), "as many rows"), (dict(q=None), "null"), (dict(lengths=None), "null"), (dict(out=None), "null"), (dict(ldq=511), "pitch"),
     (dict(ldo=8), "pitch"), (dict(mask=A, ldm=127), "pitch"), (dict(keys=P((1 << 20) + 2)), "aligned"), (dict(out=P(4097)), "aligned"),
     (dict(out=A), "out is q"), (dict(max_pages=1 << 16, max_length=1 << 20, ldt=1 << 16), "workspace"),
@@ -141,6 +142,8 @@ def test_sizes():
         assert lib.dycl_op_attend_workspace(n, 8, 2, 64, 1 << 16, 0) == 0
     long, windowed = (lib.dycl_op_attend_workspace(4, 8, 2, 64, 1 << 20, w) for w in (0, 2000))
     assert long > windowed > 0
+    for all_of_it in (1 << 20, (1 << 63) - 1):                                   # a window that is none
+        assert lib.dycl_op_attend_workspace(4, 8, 2, 64, 1 << 20, all_of_it) == long
     assert lib.dycl_op_attend_workspace(8, 8, 2, 64, 1 << 20, 0) == 2 * long
     assert lib.dycl_op_beam_workspace(0, 4, 1000, 4) == lib.dycl_op_beam_workspace(2, 65, 1000, 4) == 0
     assert lib.dycl_op_beam_workspace(2, 4, 1000, 4) >= 8 * (4 * 8 + 8)

@@ -186,7 +186,7 @@ def test_append_bad_places(de):
 # ---- attend --------------------------------------------------------------------
 
 def check_attend(de, lengths, q_heads, heads, dim, page, window=0, holes=0.0, max_length=None, scale=None, pad=0, big=1.0, rows=64):
-    g = gen(sum(lengths) + q_heads * dim + window)
+    g = gen(sum(lengths) + q_heads * dim + window % 2**31)
     cache, tables = paged(g, lengths, heads, page, dim)
     n, cap = len(lengths), tables.shape[1] * page
     for r in range(n):
@@ -238,7 +238,7 @@ def test_attend_lengths(de, length):
     check_attend(de, [length, length - 1], 4, 1, 128, 64, holes=0.1)
 
 
-@pytest.mark.parametrize("window", [1, 7, 32, 33, 100, 128, 1000, 4096, 5000, 100000])
+@pytest.mark.parametrize("window", [1, 7, 32, 33, 100, 128, 1000, 4096, 5000, 100000, 2**63 - 1])
 def test_attend_window(de, window):
     check_attend(de, [0, 1, 31, 100, 500, 3000, 6001], 4, 2, 64, 16, window=window)
     check_attend(de, [5, 777], 2, 2, 128, 8, window=window, holes=0.3)
