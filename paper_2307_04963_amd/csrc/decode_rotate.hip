@@ -351,7 +351,7 @@ void decode_rotate(const RotateArgs& a, hipStream_t stream) {
   // Rows of a tile, fewer where they would not fill the CUs: about two units per lane (16383 rows of 20 heads of 96 in float32:
   // 41 us with a row of 480 units each, 44 to 50 with 2 to 8), and with a cache more, for each tile waits for its
   // rows' pages (6000 rows of 48 heads of 128 in bf16: 31 us with a row of 384 units each, 26 with 6 or 8).
-  int64_t rows = (whole ? (a.k ? 3072 : 512) * (most / wide) : 1024) / of_row;
+  int64_t rows = (whole ? (a.k ? 2560 : 512) * (most / wide) : 1024) / of_row;
   if (a.pairs) rows = std::min<int64_t>(rows, kTableSize / a.pairs);
   rows = std::max<int64_t>(1, std::min<int64_t>({rows, kMaxRows, a.n / (a.k ? 512 : 1024)}));
   const Units u{static_cast<int>(rows), turned, copied, plain, of_q, of_row, Divide(of_row), Divide(turned + copied), Divide(plain),
