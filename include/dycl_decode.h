@@ -127,7 +127,9 @@ int dycl_op_attend(const uint16_t* q, int64_t ldq, int64_t n, int q_heads, int h
  *              fewer than k candidates are there (token -1, score -infinity, ended 0).
  *   tokens     [sequences][k] int32.   new_scores  [sequences][k] float32.
  *   new_ended  [sequences][k] uint8: the parent had ended, or the token is `end`.
- * float32; the sum's order depends on words alone.
+ * float32; the sum's order depends on words alone.  Candidates are compared as rounded to
+ * float32: of two that round to the same value either may be taken or come first, unless
+ * their logits are the same.
  *   workspace  dycl_op_beam_workspace(...) bytes, 16-byte aligned.
  * 1 <= beams <= 64, 1 <= k <= 64, 1 <= words <= 2^20, sequences * beams < 2^24.
  */

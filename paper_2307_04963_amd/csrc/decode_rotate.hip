@@ -41,10 +41,10 @@ __device__ __forceinline__ float2 turn(int32_t position, double frequency) {
   return make_float2(n == 1 || n == 2 ? -cc : cc, n >= 2 ? -ss : ss);
 }
 
-// x / d for x * d < 2^32, m = ceil(2^32 / d) (d > 1; 0 stands for d = 1)
+// x / d for x * d < 2^32, m = ceil(2^32 / d) (d > 1; 0 stands for d = 1, 1 for quotients that are all 0)
 struct Divide {
   uint32_t m;
-  explicit Divide(int d) : m(d > 1 ? static_cast<uint32_t>(((uint64_t(1) << 32) + d - 1) / d) : 0) {}
+  explicit Divide(int d, bool below = false) : m(below ? 1 : d > 1 ? static_cast<uint32_t>(((uint64_t(1) << 32) + d - 1) / d) : 0) {}
   __device__ int operator()(int x) const { return m ? static_cast<int>(__umulhi(static_cast<uint32_t>(x), m)) : x; }
 };
 
@@ -354,7 +354,8 @@ void decode_rotate(const RotateArgs& a, hipStream_t stream) {
   int64_t rows = (whole ? (a.k ? 2560 : 512) * (most / wide) : 1024) / of_row;
   if (a.pairs) rows = std::min<int64_t>(rows, kTableSize / a.pairs);
   rows = std::max<int64_t>(1, std::min<int64_t>({rows, kMaxRows, a.n / (a.k ? 512 : 1024)}));
-  const Units u{static_cast<int>(rows), turned, copied, plain, of_q, of_row, Divide(of_row), Divide(turned + copied), Divide(plain),
+  // (a row may have 98304 units, q's, k's and v's 65536 values in pairs: the square passes 2^32, but then the tile is one row)
+  const Units u{static_cast<int>(rows), turned, copied, plain, of_q, of_row, Divide(of_row, rows == 1), Divide(turned + copied), Divide(plain),
                 Divide(std::max(1, a.pairs))};
   const dim3 grid(static_cast<unsigned>(std::min((a.n + rows - 1) / rows, kMaxGrid)));
   if (a.f32 && wide == 4 && whole)

@@ -151,6 +151,13 @@ def test_append_heads_and_rows(de):
     check_append(de, [1100, 13], [0, 0], 2, 1, 64, 16, "interleaved", 16, B, shuffle=False)
 
 
+@pytest.mark.parametrize("heads", [8152, 8192])
+def test_append_widest(de, heads):
+    """Rows of 97824 and 98304 units of two values: the last ones belong to the same row."""
+    for dtype in (B, F):
+        check_append(de, [1, 2], [0, 7], heads, heads, 8, 1, "interleaved", 8, dtype)
+
+
 def test_append_one_token_per_sequence(de):
     """Without `sequence` row r is sequence r; without q nothing is returned; q_out may be q."""
     g = gen(9)
