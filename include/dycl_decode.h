@@ -100,7 +100,7 @@ int dycl_op_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const
  *   window        0 (none) or the number of last places seen.
  *   workspace     dycl_op_attend_workspace(...) bytes, 16-byte aligned, or NULL when that is 0.
  * Scores, softmax and sums are float32.  The softmax's weights enter the second product as
- * two bf16 terms (16 significant bits).  The keys are summed in parts that the
+ * three bf16 terms, all of float32's 24 significant bits.  The keys are summed in parts that the
  * dim alone sets, joined in a fixed order.  -1e38 < scale < 1e38,
  * q_heads a multiple of heads, n * q_heads < 2^31, max_length < 2^31 - 4096.
  */

@@ -310,24 +310,27 @@ __global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_ke
     }
     m = other_rows_max(top);
     const float all = m == kNone ? 0.f : m;
-    // The weights in two terms (a single bf16 would be off by up to 2^-8 of each): the first is
-    // the weight cut off after 8 bits, the second the rest, never 0, so that a seen key's infinite value
-    // stays one where 0 times it would be NaN; 2^-126 of a value is below its sum's rounding.
+    // The weights in three terms, each the next 8 bits cut off: together float32's 24.  (Two would be off by up to 2^-17 of each weight, one
+    // by 2^-8.)  The second and third are never 0, so that a seen key's infinite value stays one where 0 times it would be NaN.
     constexpr float kLeast = 1.17549435e-38f;
-    bf16x8 p_hi[U], p_lo[U];
+    auto high = [](float a) { return __uint_as_float(__float_as_uint(a) & 0xffff0000u); };
+    auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+    bf16x8 weights[3][U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      uint32_t ph[4], pl[4];
+      uint32_t bits[3][4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float a = __builtin_amdgcn_exp2f(s[u][2 * j] - all), b = __builtin_amdgcn_exp2f(s[u][2 * j + 1] - all);
         l += a;
         l += b;
-        ph[j] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-        pl[j] = pack_bf16(fmaxf(a - __uint_as_float(ph[j] << 16), kLeast), fmaxf(b - __uint_as_float(ph[j] & 0xffff0000u), kLeast));
+        const float a1 = fmaxf(a - high(a), kLeast), b1 = fmaxf(b - high(b), kLeast);
+        bits[0][j] = pair(a, b);
+        bits[1][j] = pair(a1, b1);
+        bits[2][j] = pair(fmaxf(a1 - high(a1), kLeast), fmaxf(b1 - high(b1), kLeast));
       }
-      p_hi[u] = __builtin_bit_cast(bf16x8, make_uint4(ph[0], ph[1], ph[2], ph[3]));
-      p_lo[u] = __builtin_bit_cast(bf16x8, make_uint4(pl[0], pl[1], pl[2], pl[3]));
+#pragma unroll
+      for (int w = 0; w < 3; ++w) weights[w][u] = __builtin_bit_cast(bf16x8, make_uint4(bits[w][0], bits[w][1], bits[w][2], bits[w][3]));
     }
 #pragma unroll
     for (int h = 0; h < VH; ++h)
@@ -340,8 +343,8 @@ __global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_ke
 #pragma unroll
           for (int j = 0; j < 4; ++j) a[j] = __builtin_amdgcn_perm(vr[u][2 * j + 1][h][i / 2], vr[u][2 * j][h][i / 2], pick[u][i & 1][j]);
           const bf16x8 v = __builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3]));
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_hi[u], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_lo[u], acc, 0, 0, 0);
+#pragma unroll
+          for (int w = 0; w < 3; ++w) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, weights[w][u], acc, 0, 0, 0);
         }
         if (i & 1) __builtin_amdgcn_sched_barrier(0);      // (else all operands are made first, in registers that there are not)
       }

@@ -1,0 +1,56 @@
+"""The decoding operators' values where few bits or a number's range decide them: weights that nearly cancel, values near the
+type's largest, weights that vanish, large logits."""
+
+import pytest
+import torch
+
+from tests._decode import ROUND, UNIT, within
+
+pytestmark = pytest.mark.gpu
+
+B, F = torch.bfloat16, torch.float32
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def de():
+    assert torch.cuda.is_available()
+    from paper_2307_04963_amd import decoding
+    return decoding
+
+
+# Capacities for which a workgroup takes a part, a run and a stretch of the keys where there are a thousand rows.
+CAPACITIES = [8, 1024, 2048]
+
+
+def attend(de, scores, values, dim, capacity):
+    """Rows of 8 keys: row r's key j has the score scores[r, j] (bf16 values) and values[r, j] in every column -> [rows, dim]."""
+    rows = scores.shape[0]
+    assert scores.shape == values.shape == (rows, 8)
+    cache = de.Cache(*(torch.zeros((rows, 1, 8, dim), dtype=B, device="cuda") for _ in range(2)))
+    cache.keys[:, 0, :, 3] = scores.to(B)
+    cache.values[:] = values.to(B)[:, None, :, None]
+    tables = torch.full((rows, capacity // 8), -1, dtype=torch.int32, device="cuda")
+    tables[:, 0] = torch.arange(rows, dtype=torch.int32, device="cuda")
+    q = torch.zeros((rows, dim), dtype=B, device="cuda")
+    q[:, 3] = 1
+    return de.attend(q, cache, tables, torch.full((rows,), 8, dtype=torch.int32, device="cuda"), scale=1.0)
+
+
+@pytest.mark.parametrize("capacity", CAPACITIES)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_weights_have_24_bits(de, dim, capacity):
+    """Two keys of weights 1 and e^s, values -c and 1 with c next to e^s: what is left is as exact as float32's weights are.
+
+    Off by, in units of 2^-24 of the sum of p |v|: the score in base 2, two roundings of 1.45 |s| at most, 2; the exponential, 2^-22: 4;
+    the products' and the weights' sums, the quotient and its product, 8.  The others of the eight keys have no weight."""
+    s = torch.cat([torch.arange(128, 256, device="cuda") * -(2.0 ** (e - 8)) for e in range(-6, 1)])
+    s = torch.cat([s, s[:128]])                             # a thousand rows
+    scores = torch.full((len(s), 8), -INF, device="cuda")
+    values = torch.zeros_like(scores)
+    c = s.double().exp().to(B)
+    scores[:, 0], scores[:, 1], values[:, 0], values[:, 1] = 0, s, -c.float(), 1
+    p = s.double().exp()
+    want = ((p - c.double()) / (1 + p))[:, None].expand(-1, dim)
+    size = ((p + c.double()) / (1 + p))[:, None]
+    within(attend(de, scores, values, dim, capacity), want, 14 * UNIT * size + ROUND * want.abs())
