@@ -311,8 +311,9 @@ __global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_ke
     m = other_rows_max(top);
     const float all = m == kNone ? 0.f : m;
     // The weights in three terms, each the next 8 bits cut off: together float32's 24.  (Two would be off by up to 2^-17 of each weight, one
-    // by 2^-8.)  The second and third are never 0, so that a seen key's infinite value stays one where 0 times it would be NaN.
-    constexpr float kLeast = 1.17549435e-38f;
+    // by 2^-8.)  The second and third are at least 2^-30 of the weight and so not 0 where it is not (from 2^-96 of the largest on), so that a
+    // seen key's infinite value stays one where 0 times it would be NaN; a weight of 0 adds nothing, however large the value.
+    constexpr float kLeast = 9.31322574615478515625e-10f;
     auto high = [](float a) { return __uint_as_float(__float_as_uint(a) & 0xffff0000u); };
     auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
     bf16x8 weights[3][U];
@@ -324,10 +325,11 @@ __global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_ke
         const float a = __builtin_amdgcn_exp2f(s[u][2 * j] - all), b = __builtin_amdgcn_exp2f(s[u][2 * j + 1] - all);
         l += a;
         l += b;
-        const float a1 = fmaxf(a - high(a), kLeast), b1 = fmaxf(b - high(b), kLeast);
+        const float a_least = a * kLeast, b_least = b * kLeast;
+        const float a1 = fmaxf(a - high(a), a_least), b1 = fmaxf(b - high(b), b_least);
         bits[0][j] = pair(a, b);
         bits[1][j] = pair(a1, b1);
-        bits[2][j] = pair(fmaxf(a1 - high(a1), kLeast), fmaxf(b1 - high(b1), kLeast));
+        bits[2][j] = pair(fmaxf(a1 - high(a1), a_least), fmaxf(b1 - high(b1), b_least));
       }
 #pragma unroll
       for (int w = 0; w < 3; ++w) weights[w][u] = __builtin_bit_cast(bf16x8, make_uint4(bits[w][0], bits[w][1], bits[w][2], bits[w][3]));

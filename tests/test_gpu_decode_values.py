@@ -1,6 +1,8 @@
 """The decoding operators' values where few bits or a number's range decide them: weights that nearly cancel, values near the
 type's largest, weights that vanish, large logits."""
 
+import math
+
 import pytest
 import torch
 
@@ -54,3 +56,27 @@ def test_attend_weights_have_24_bits(de, dim, capacity):
     want = ((p - c.double()) / (1 + p))[:, None].expand(-1, dim)
     size = ((p + c.double()) / (1 + p))[:, None]
     within(attend(de, scores, values, dim, capacity), want, 14 * UNIT * size + ROUND * want.abs())
+
+
+@pytest.mark.parametrize("capacity", CAPACITIES)
+@pytest.mark.parametrize("dim", [64, 72, 128, 256])
+def test_attend_values_without_weight(de, dim, capacity):
+    """Finite values as large as they come add what their weights say, and nothing without one; infinite ones are."""
+    n, no = 0.0, -INF
+    big = torch.tensor(3e38).to(B).item()
+    rows = [([n, no, no, no, no, no, no, no], [1, big, 0, 0, 0, 0, 0, 0], 1.0),        # a score of -infinity
+            ([n, -200, no, no, no, no, no, -200], [1, big, 0, 0, 0, 0, 0, -big], 1.0),  # e^-200
+            ([n, -60, no, no, no, no, no, no], [1, big, 0, 0, 0, 0, 0, 0], (1 + big * math.exp(-60)) / (1 + math.exp(-60))),
+            ([no] * 8, [big] * 8, 0.0),
+            # an infinite value is one, whatever bits its weight has
+            ([n, no, no, no, no, no, no, no], [INF, 0, 0, 0, 0, 0, 0, 0], INF),
+            ([n, n, -1, -20, no, no, no, no], [1, -INF, 1, 1, 0, 0, 0, 0], -INF),
+            ([n, n, -1, -30, no, no, no, no], [1, 1, 1, INF, 0, 0, 0, 0], INF)]
+    times = 1024 // len(rows) + 1
+    scores, values = (torch.tensor([r[i] for r in rows], device="cuda").repeat(times, 1) for i in (0, 1))
+    got = attend(de, scores, values, dim, capacity)
+    assert torch.equal(got, got[:len(rows)].repeat(times, 1))
+    for r, (_, _, want) in enumerate(rows):
+        # (a score of 60 is off by up to 120 * 2^-24 where it is taken to base 2, and so is its weight)
+        bound = 0.0 if want in (1.0, 0.0, INF, -INF) else want * (ROUND + 2.0 ** -15)
+        assert all(v == want or abs(v - want) <= bound for v in got[r].tolist()), (r, got[r, 0].item(), want)
