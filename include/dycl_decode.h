@@ -86,8 +86,8 @@ int dycl_op_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const
  * (from 0 without a window) whose mask is not 0.  Query head h reads the
  * cache's head h / (q_heads / heads).  A key whose score is -infinity has
  * weight 0 and adds nothing, however large its value.  (An infinite value makes its column's result
- * infinite where its key's weight is 2^-64 of the row's largest or more, and infinite or NaN where it is less.)  A row without
- * a key is 0.  What the cache holds in places that a row does not see is not used, whatever it is.
+ * infinite where its key's weight is 2^-64 of the row's largest or more, and infinite or NaN where it is less; weights below 2^-94 of
+ * it may count as 0.)  A row without a key is 0.  What the cache holds in places that a row does not see is not used, whatever it is.
  *   q, out        [n][q_heads * dim] bf16; out may not be q.
  *   lengths       [n] int32: keys that the row sees.  Below 0 as 0, past
  *                 max_length as max_length.

@@ -87,7 +87,7 @@ __device__ __forceinline__ uint32_t open_of(const uint8_t* mask, int64_t key, in
   return open;
 }
 
-// Four values' weighted sums over some keys: of exp2(score - top) * value, and of the weights alone.
+// Four values' weighted sums over some keys: of exp2(score - top) * value, scaled as the row's weights are, and of the weights alone.
 struct Sum {
   float4 v;
   float top, total;
@@ -184,6 +184,11 @@ __global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_ke
   if (d.pieces > 1 && first >= span.hi) return;       // (the same for the whole workgroup)
   here_lane &= page_lane < 0 ? 0u : octet_of(span, key_lane);
   page_lane = max(page_lane, 0);                     // (read, if at all, and not used)
+
+  // Weights are scaled by a power of two that keeps their sum, over all keys of the row, below 1: sums of values then stay within the
+  // largest of them, and what follows is divided by the weights' sum anyway.
+  const int bits = 64 - __clzll(static_cast<unsigned long long>(max(int64_t(0), span.hi - span.lo)));
+  const float down = __uint_as_float(static_cast<uint32_t>(127 - bits) << 23);
 
   const int parts = MANY ? static_cast<int>(max(int64_t(1), min(static_cast<int64_t>(take), (span.hi - first + S::kPart - 1) / S::kPart))) : 1;
   // (a tile without keys of its row has none behind it)
@@ -311,7 +316,7 @@ __global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_ke
     m = other_rows_max(top);
     const float all = m == kNone ? 0.f : m;
     // The weights in three terms, each the next 8 bits cut off: together float32's 24.  (Two would be off by up to 2^-17 of each weight, one
-    // by 2^-8.)  The second and third are at least 2^-30 of the weight and so not 0 where it is not (from 2^-96 of the largest on), so that a
+    // by 2^-8.)  The second and third are at least 2^-30 of the weight and so not 0 where it is not (from 2^-64 of the largest on), so that a
     // seen key's infinite value stays one where 0 times it would be NaN; a weight of 0 adds nothing, however large the value.
     constexpr float kLeast = 9.31322574615478515625e-10f;
     auto high = [](float a) { return __uint_as_float(__float_as_uint(a) & 0xffff0000u); };
@@ -322,7 +327,7 @@ __global__ __launch_bounds__(kThreads, MANY && DP <= 128 ? 3 : 2) void attend_ke
       uint32_t bits[3][4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float a = __builtin_amdgcn_exp2f(s[u][2 * j] - all), b = __builtin_amdgcn_exp2f(s[u][2 * j + 1] - all);
+        const float a = __builtin_amdgcn_exp2f(s[u][2 * j] - all) * down, b = __builtin_amdgcn_exp2f(s[u][2 * j + 1] - all) * down;
         l += a;
         l += b;
         const float a_least = a * kLeast, b_least = b * kLeast;

@@ -11,7 +11,7 @@ from tests._decode import ROUND, UNIT, within
 pytestmark = pytest.mark.gpu
 
 B, F = torch.bfloat16, torch.float32
-INF = float("inf")
+INF, MOST = float("inf"), torch.finfo(torch.bfloat16).max
 
 
 @pytest.fixture(scope="module")
@@ -80,3 +80,27 @@ def test_attend_values_without_weight(de, dim, capacity):
         # (a score of 60 is off by up to 120 * 2^-24 where it is taken to base 2, and so is its weight)
         bound = 0.0 if want in (1.0, 0.0, INF, -INF) else want * (ROUND + 2.0 ** -15)
         assert all(v == want or abs(v - want) <= bound for v in got[r].tolist()), (r, got[r, 0].item(), want)
+
+
+@pytest.mark.parametrize("capacity", CAPACITIES)
+@pytest.mark.parametrize("dim", [64, 72, 128, 256])
+def test_attend_largest_values(de, dim, capacity):
+    """Sums of the type's largest values do not pass its range: a mean of equal values is that value."""
+    n, no = 0.0, -INF
+    rows = [([n] * 8, [MOST] * 8, MOST), ([n, n, no, no, no, no, no, no], [-MOST, -MOST, 0, 0, 0, 0, 0, 0], -MOST),
+            ([n] * 8, [MOST, -MOST] * 4, 0.0), ([n, n, n, no, no, no, no, n], [MOST, MOST, -MOST, 0, 0, 0, 0, MOST], MOST / 2)]
+    scores, values = (torch.tensor([r[i] for r in rows], device="cuda").repeat(256, 1) for i in (0, 1))
+    got = attend(de, scores, values, dim, capacity)
+    for r, (_, _, want) in enumerate(rows):
+        assert bool((got[r::len(rows)] == want).all()), (r, got[r, 0].item(), want)
+
+
+@pytest.mark.parametrize("q_heads", [1, 2, 20])
+def test_attend_many_largest_values(de, q_heads):
+    """5000 and 70000 keys of the largest value, more than a stretch: their mean is that value."""
+    for dim, length in ((64, 5000), (128, 5000), (64, 70000)):
+        pages = length // 8
+        cache = de.Cache(torch.zeros((pages, 1, 8, dim), dtype=B, device="cuda"), torch.full((pages, 1, 8, dim), MOST, dtype=B, device="cuda"))
+        tables = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(3, 1)
+        lengths = torch.tensor([length, length - 1, 1], dtype=torch.int32, device="cuda")
+        assert bool((de.attend(torch.ones((3, q_heads * dim), dtype=B, device="cuda"), cache, tables, lengths) == MOST).all())
