@@ -20,7 +20,7 @@ namespace k {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kRoom = 512;
-constexpr float kClosed = -__builtin_inff(), kLog2e = 1.44269504088896340736f, kLargest = 3.402823466e38f;
+constexpr float kClosed = -__builtin_inff(), kLog2e = 1.44269504088896340736f, kLargest = 3.402823466e38f, kFar = 1e6f;
 
 // a value and an index as one number: larger values first, then lower indices; 0 is none
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -155,13 +155,13 @@ __global__ __launch_bounds__(kThreads) void segment_kernel(BeamArgs p, Segments 
   };
   maxima();
   // Ordinary values: 2^(v log2 e - a) by one multiplication and addition, a the rounded m log2 e, and what that
-  // rounding took put right at the end.
+  // rounding took, less than 2^-3 up to kFar, put right at the end.  (From 10^9 on it passes the exponential's range.)
   const float a = m == kClosed ? 0.f : m * kLog2e;
 #pragma unroll
   for (int i = 0; i < 8 * V; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i], kLog2e, -a));
   if (m != kClosed) sum *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, kLog2e, -a));
-  if (__any(!(sum < kLargest)) || (m != kClosed && !(fabsf(m) < 1e30f))) {
-    // NaN among them, which is closed, +infinity, which is the largest finite value, or a product beyond it
+  if (__any(!(sum < kLargest)) || (m != kClosed && !(fabsf(m) < kFar))) {
+    // NaN among them, which is closed, +infinity, which is the largest finite value, or values far from 0
 #pragma unroll
     for (int i = 0; i < 8 * V; ++i) v[i] = fminf(fmaxf(v[i], kClosed), kLargest);
     maxima();

@@ -104,3 +104,24 @@ def test_attend_many_largest_values(de, q_heads):
         tables = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(3, 1)
         lengths = torch.tensor([length, length - 1, 1], dtype=torch.int32, device="cuda")
         assert bool((de.attend(torch.ones((3, q_heads * dim), dtype=B, device="cuda"), cache, tables, lengths) == MOST).all())
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("low, high", [(1e5, 1e6), (1e6, 1e9), (1.4e9, 3e9), (3e9, 1e12), (1e29, 1e31), (1e37, 3e38)])
+def test_beam_large_logits(de, low, high, sign, dtype):
+    """Rows whose largest logit is far above the others: it alone is likely, its value is the beam's score."""
+    g = torch.Generator(device="cuda").manual_seed(int(low) % 1000003 + sign)
+    rows, words = 4096, 300
+    top = sign * torch.exp(math.log(low) + (math.log(high) - math.log(low)) * torch.rand(rows, generator=g, device="cuda"))
+    at = torch.randint(0, words, (rows,), generator=g, device="cuda")
+    less = torch.rand((rows, words), generator=g, device="cuda") * 0.4 + 0.05           # by 5 to 45 percent
+    logits = (top[:, None] - less * top.abs()[:, None]).to(dtype)
+    logits.scatter_(1, at[:, None], top.to(dtype)[:, None])
+    scores = -9 * torch.rand(rows, generator=g, device="cuda")
+    got = de.beam(logits, scores, 1, k=1)
+    assert torch.equal(got.tokens[:, 0].long(), at) and torch.equal(got.parents[:, 0].long(), torch.arange(rows, device="cuda"))
+    # The others' exponentials are 0, the logarithm of 1 is.  Where the largest is taken around its rounded product, its own exponential
+    # and what puts that right are each 2^-22 off, their product 2^-24, so the logarithm is off by 2^-21 + 2^-24 at most, and
+    # the two sums that it enters by a rounding each.
+    within(got.scores[:, 0], scores.double(), 2.0 ** -21 + UNIT + 2 * UNIT * scores.double().abs())
