@@ -46,7 +46,8 @@ def frequencies(dims: int, base: float = 10000.0, *, scaling: str = "none", fact
     "base"     base * factor^(dims / (dims - 2)): the slowest pair divided by factor, the fastest kept
     "turns"    by the turns t = trained * f / (2 pi) that a pair makes in the trained context: f from `fast` turns on,
                f / factor up to `slow`, between them the blend of the two, linear in t
-    "pairs"    the same with the blend linear in i, from the pair that makes `fast` turns to the one that makes `slow`
+    "pairs"    the same with the blend linear in i, from the pair that makes `fast` turns (rounded down) to the one that makes
+               `slow` (rounded up), wherever these lie, also outside the dims / 2 pairs
     """
     if dims < 2 or dims % 2:
         raise ValueError("dims must be even and at least 2")
@@ -66,11 +67,11 @@ def frequencies(dims: int, base: float = 10000.0, *, scaling: str = "none", fact
         if scaling == "turns":
             keep = (trained * f / (2 * math.pi) - slow) / (fast - slow)
         else:
-            # the pair that makes t turns: trained * base^(-2 i / dims) = 2 pi t
+            if base <= 1:
+                raise ValueError('scaling "pairs" needs a base above 1')
+            # the pair that makes t turns: trained * base^(-2 i / dims) = 2 pi t; it may lie before the first pair or past the last
             of = lambda t: dims * math.log(trained / (2 * math.pi * t)) / (2 * math.log(base))  # noqa: E731
-            if base == 1:
-                raise ValueError('scaling "pairs" needs a base other than 1')
-            first, last = max(math.floor(of(fast)), 0), min(math.ceil(of(slow)), dims // 2 - 1)
+            first, last = math.floor(of(fast)), math.ceil(of(slow))
             keep = 1 - (i - first) / max(last - first, 1e-3)
         keep = keep.clamp(0, 1)
         f = f * (keep + (1 - keep) / factor)
