@@ -151,6 +151,7 @@ int dycl_op_beam(const void* logits, int type, int64_t ldl, const float* scores,
  *   new_tables  [n][max_pages] (pitch ldn), new_lengths [n]; NULL: not written, only the pages
  *               are (for a further layer with the same tables).
  *   keys, values  one layer's cache, or both NULL: only tables and lengths.
+ * n == 0 does nothing, but refuses a cache that is refused otherwise: a caller of several layers can check all before the first.
  */
 int dycl_op_fork(const int32_t* tables, int64_t ldt, const int32_t* lengths, int64_t rows, int max_pages,
                  const int32_t* parents, const int32_t* fresh, int64_t n, int32_t* new_tables, int64_t ldn,

@@ -260,14 +260,15 @@ int dycl_op_fork(const int32_t* tables, int64_t ldt, const int32_t* lengths, int
     need((keys == nullptr) == (values == nullptr), op, "keys and values are given together");
     need((new_tables == nullptr) == (new_lengths == nullptr), op, "new tables and lengths are given together");
     need_sizes(op, keys ? heads : 1, page, keys ? dim : 8, max_pages, keys ? pages : 1, rows);
+    need(at(keys, 16) && at(values, 16), op, kUnaligned);
+    need(!keys || keys != values, op, "keys are the values");
     if (n == 0) return static_cast<int>(DYCL_OK);
     need(keys || new_tables, op, "neither a cache nor new tables");
     need(((tables && lengths) || rows == 0) && parents && fresh, op, "null tables, lengths, parents or fresh");
     need(pitch_ok(ldt, max_pages) && (!new_tables || pitch_ok(ldn, max_pages)), op, "a row pitch below the row");
-    need(at(tables, 4) && at(lengths, 4) && at(parents, 4) && at(fresh, 4) && at(new_tables, 4) && at(new_lengths, 4) &&
-             at(keys, 16) && at(values, 16),
-         op, kUnaligned);
-    need(new_tables != tables && new_lengths != lengths && (!keys || keys != values), op, "new tables or lengths are the old ones, or keys the values");
+    need(at(tables, 4) && at(lengths, 4) && at(parents, 4) && at(fresh, 4) && at(new_tables, 4) && at(new_lengths, 4), op,
+         kUnaligned);
+    need(new_tables != tables && new_lengths != lengths, op, "new tables or lengths are the old ones");
     ForkArgs a{};
     a.cache = paged(keys, values, pages, keys ? heads : 1, page, keys ? dim : 8, tables, ldt, rows, max_pages);
     a.lengths = lengths;

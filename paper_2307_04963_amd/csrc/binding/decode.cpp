@@ -1,6 +1,8 @@
 // Python entry points of the decoding operators (include/dycl_decode.h); decoding.py
 // gives their arguments names and defaults.
+#include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "tensors.hpp"
 
@@ -231,16 +233,19 @@ PyObject* beam(PyObject*, PyObject* const* args, Py_ssize_t count) {
   });
 }
 
-// keys or None, values or None, page, tables, lengths, parents, fresh, out_tables, out_lengths, write (0: only the pages) -> (tables, lengths)
+// tables, lengths, parents, fresh, page or None, out_tables, out_lengths, then each layer's keys and values -> (tables, lengths).
+// Everything about every layer is checked before the first layer's launch.
 PyObject* fork(PyObject*, PyObject* const* args, Py_ssize_t count) {
   return guarded([&] {
-    Args a(args, count, 10);
-    const at::Tensor *keys = a.tensor("cache.keys"), *values = a.tensor("cache.values");
-    int page = a.small("page");
+    Args a(args, count, std::max<Py_ssize_t>(count, 7));
     const at::Tensor &tables = *a.tensor("tables", false), &lengths = *a.tensor("lengths", false);
     const at::Tensor &parents = *a.tensor("parents", false), &fresh = *a.tensor("fresh", false);
+    const bool has_page = *a.a != Py_None;
+    int page = has_page ? a.small("page") : (a.next(), 0);
     const at::Tensor *out_tables = a.tensor("out_tables"), *out_lengths = a.tensor("out_lengths");
-    const bool write = a.integer() != 0;
+    std::vector<Cache> layers;
+    if (a.left % 2) refuse("a layer's cache must be its keys and values");
+    while (a.left) layers.emplace_back(a);
 
     if (!tables.is_cuda()) refuse("tables must be on a GPU");
     const at::Device dev = tables.device();
@@ -251,31 +256,29 @@ PyObject* fork(PyObject*, PyObject* const* args, Py_ssize_t count) {
     const int32_t* len = ints(&lengths, "lengths", {table.sequences}, dev);
     if (fresh.numel() != n || fresh.scalar_type() != at::kInt || !fresh.is_contiguous() || fresh.device() != dev)
       refuse("fresh must be a contiguous int32 tensor like parents");
-    int64_t pages = 0;
-    int heads = 0, dim = 0;
-    if (keys) {
-      if (!values) refuse("cache.values must be like cache.keys");
-      PyObject* const both[2] = {args[0], args[1]};
-      Args again(both, 2, 2);
-      Cache cache(again);
-      cache.check(dev);
-      pages = cache.pages, heads = cache.heads, page = cache.page, dim = cache.dim;
+    for (Cache& c : layers) {
+      c.check(dev);
+      // (its pointers would be null, which to the C interface is no cache)
+      if (!c.keys->numel()) refuse("the cache is empty");
+      if (has_page && c.page != page) refuse("page is not the cache's");
+      if (c.page != layers[0].page) refuse("the layers' pages must hold the same number of tokens");
     }
+    if (!layers.empty()) page = layers[0].page;
     const c10::DeviceGuard on(dev);
-    at::Tensor t, l;
-    int64_t ldn = table.max_pages;
-    if (write) {
-      t = out_tables ? *out_tables : make({n, table.max_pages}, at::kInt, dev);
-      l = out_lengths ? *out_lengths : make({n}, at::kInt, dev);
-      const Tables next(t, dev);
-      ldn = next.ld;
-      if (t.size(0) != n || next.max_pages != table.max_pages) refuse("out_tables must be " + sizes(n, table.max_pages));
-      ints(&l, "out_lengths", {n}, dev);
-    }
-    check(dycl_op_fork(table.data, table.ld, len, table.sequences, table.max_pages, static_cast<const int32_t*>(parents.data_ptr()),
-                       static_cast<const int32_t*>(fresh.data_ptr()), n, write ? static_cast<int32_t*>(t.data_ptr()) : nullptr, ldn,
-                       write ? static_cast<int32_t*>(l.data_ptr()) : nullptr, bits(keys), bits(values), pages, heads, page, dim,
-                       stream_of(dev)));
+    at::Tensor t = out_tables ? *out_tables : make({n, table.max_pages}, at::kInt, dev);
+    at::Tensor l = out_lengths ? *out_lengths : make({n}, at::kInt, dev);
+    const Tables next(t, dev);
+    if (t.size(0) != n || next.max_pages != table.max_pages) refuse("out_tables must be " + sizes(n, table.max_pages));
+    ints(&l, "out_lengths", {n}, dev);
+    auto call = [&](const Cache* c, int64_t rows, bool write) {
+      check(dycl_op_fork(table.data, table.ld, len, table.sequences, table.max_pages, static_cast<const int32_t*>(parents.data_ptr()),
+                         static_cast<const int32_t*>(fresh.data_ptr()), rows, write ? static_cast<int32_t*>(t.data_ptr()) : nullptr, next.ld,
+                         write ? static_cast<int32_t*>(l.data_ptr()) : nullptr, c ? bits(c->keys) : nullptr, c ? bits(c->values) : nullptr,
+                         c ? c->pages : 0, c ? c->heads : 0, page, c ? c->dim : 0, stream_of(dev)));
+    };
+    for (size_t i = 1; i < layers.size(); ++i) call(&layers[i], 0, false);     // (no rows: only its checks)
+    call(layers.empty() ? nullptr : &layers[0], n, true);
+    for (size_t i = 1; i < layers.size(); ++i) call(&layers[i], n, false);
     return tuple({t, l});
   });
 }

@@ -136,16 +136,4 @@ def fork(cache, tables: torch.Tensor, lengths: torch.Tensor, parents: torch.Tens
     layers = [cache] if isinstance(cache, Cache) else list(cache or [])
     if not layers and page is None:
         raise ValueError("without a cache, page (tokens of a page) must be given")
-    if page is not None and any(c.keys.dim() == 4 and c.keys.shape[2] != page for c in layers):
-        raise ValueError("page is not the cache's")
-    if len({c.keys.shape[2:3] for c in layers}) > 1:
-        raise ValueError("the layers' pages must hold the same number of tokens")
-
-    def all_layers(tables, *rest):
-        got = None
-        for i, c in enumerate(layers or [Cache(None, None)]):
-            r = _tokens.fork(*c, page or 0, tables, *rest, out_tables, out_lengths, i == 0)
-            got = r if i == 0 else got
-        return got
-
-    return _call(stream, all_layers, tables, lengths, parents, fresh)
+    return _call(stream, _tokens.fork, tables, lengths, parents, fresh, page, out_tables, out_lengths, *(t for c in layers for t in c))
