@@ -7,6 +7,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
@@ -68,7 +69,9 @@ struct Args {
     if (!THPVariable_Check(o)) refuse(std::string(what) + " must be a tensor" + (optional ? " or None" : ""));
     const at::Tensor& t = THPVariable_Unpack(o);
     if (t.requires_grad() && c10::GradMode::is_enabled())
-      refuse(std::string(what) + " requires grad, and the token operators have no backward: call them under torch.no_grad(), or detach it");
+      refuse(std::string(what) + " requires grad, and these operators record no gradients: call them under torch.no_grad(), or detach it");
+    if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined())
+      refuse(std::string(what) + " carries a forward-mode tangent, which these operators would drop: give them forward_ad.unpack_dual(...).primal");
     return &t;
   }
   long integer() {

@@ -10,8 +10,9 @@ dimension is contiguous (rows may be strided: a slice of a wider product is
 taken as it is).  Work is queued on ``stream`` (default: the current one); what
 a call allocates belongs to that stream.  Wrong tensors raise ValueError, other
 refusals DyclError.  Nothing here records gradients (tensors that require
-grad are refused where gradients are recorded); rotate's ``adjoint`` is its
-gradient.
+grad are refused where gradients are recorded, and those that carry a
+forward-mode tangent); rotate's ``adjoint`` is its gradient, and rotate of a
+tangent its tangent.
 """
 
 from __future__ import annotations

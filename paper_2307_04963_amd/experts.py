@@ -8,7 +8,8 @@ Matrices are 2-D tensors whose last dimension is contiguous (rows may be
 strided).  Work is queued on ``stream`` (default: the current one); what a call
 allocates belongs to that stream.  Wrong tensors raise ValueError, other
 refusals DyclError.  Nothing here has a backward: tensors that require grad are
-refused where gradients are recorded (call under torch.no_grad()).
+refused where gradients are recorded (call under torch.no_grad()), and those
+that carry a forward-mode tangent.
 """
 
 from __future__ import annotations
