@@ -220,15 +220,19 @@ PyObject* beam(PyObject*, PyObject* const* args, Py_ssize_t count) {
                                                                   : vector<uint8_t>(ended, "ended", {rows}, at::kByte, dev);
     const int64_t sequences = rows / beams;
     const c10::DeviceGuard on(dev);
-    const at::Tensor parents = make({sequences, k}, at::kInt, dev), tokens = make({sequences, k}, at::kInt, dev);
-    const at::Tensor next = make({sequences, k}, at::kFloat, dev), over = make({sequences, k}, at::kByte, dev);
-    at::Tensor own;
-    size_t have;
     const int v = static_cast<int>(words);
-    void* ws = workspace_of(given, automatic, dycl_op_beam_workspace(sequences, beams, v, k), dev, own, have);
-    check(dycl_op_beam(logits.data_ptr(), type_of(logits), ldl, s, e, end, sequences, beams, v, k, static_cast<int32_t*>(parents.data_ptr()),
-                       static_cast<int32_t*>(tokens.data_ptr()), static_cast<float*>(next.data_ptr()),
-                       static_cast<uint8_t*>(over.data_ptr()), ws, have, stream_of(dev)));
+    const size_t bytes = dycl_op_beam_workspace(sequences, beams, v, k);
+    at::Tensor parents, tokens, next, over, own;
+    if (bytes || !sequences) {           // (else the sizes are refused: nothing is allocated for them)
+      parents = make({sequences, k}, at::kInt, dev), tokens = make({sequences, k}, at::kInt, dev);
+      next = make({sequences, k}, at::kFloat, dev), over = make({sequences, k}, at::kByte, dev);
+    }
+    auto data = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    size_t have;
+    void* ws = workspace_of(given, automatic, bytes, dev, own, have);
+    check(dycl_op_beam(logits.data_ptr(), type_of(logits), ldl, s, e, end, sequences, beams, v, k, static_cast<int32_t*>(data(parents)),
+                       static_cast<int32_t*>(data(tokens)), static_cast<float*>(data(next)), static_cast<uint8_t*>(data(over)), ws, have,
+                       stream_of(dev)));
     return tuple({parents, tokens, next, over});
   });
 }
