@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from tests._decode import ROUND, UNIT, within
+from tests._decode import ROUND, UNIT, chosen64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,28 @@ def test_beam_large_logits(de, low, high, sign, dtype):
     # and what puts that right are each 2^-22 off, their product 2^-24, so the logarithm is off by 2^-21 + 2^-24 at most, and
     # the two sums that it enters by a rounding each.
     within(got.scores[:, 0], scores.double(), 2.0 ** -21 + UNIT + 2 * UNIT * scores.double().abs())
+
+
+@pytest.mark.parametrize("words", [700, 5000, 70001])
+@pytest.mark.parametrize("offset", [0.0, -1000.0, 1e5, 3e6])
+def test_beam_scores(de, offset, words):
+    """Scores to the roundings of 32 bits, also where all of a row's logits are large.
+
+    In units of 2^-24: the exponentials 4, their arguments 0.7 log2(words) on the average: 12, their sum over 32 values of a lane, the lanes,
+    the waves and the segments 64; the logarithm and the terms' roundings 2 of the logarithm (24) and 4 of the result and of the
+    logit below the largest, which is less: 8 of the result."""
+    g = torch.Generator(device="cuda").manual_seed(words)
+    beams, k = 4, 6
+    for _ in range(50):
+        logits = 3 * torch.randn((5 * beams, words), generator=g, device="cuda") + offset
+        scores = -8 * torch.rand(5 * beams, generator=g, device="cuda")
+        parents, tokens, best, _, c = chosen64(logits, scores, beams, k)
+        top = c.sort(dim=1, descending=True).values[:, :k + 1]
+        gap = top[:, :-1] - top[:, 1:]
+        if not ((gap > 0) & (gap < 1e-4)).any():
+            break
+    else:
+        raise AssertionError("no such rows")
+    got = de.beam(logits, scores, beams, k=k)
+    assert torch.equal(got.parents, parents) and torch.equal(got.tokens, tokens)
+    within(got.scores, best, UNIT * (104 + 8 * best.abs()))
