@@ -97,7 +97,7 @@ int dycl_op_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const
  *   mask          [n][max_length] uint8, pitch ldm, or NULL.  0: the token at that place
  *                 skipped this block and has no key here.
  *   max_length    at least every length, at most max_pages * page; the work
- *                 is laid out for it (a tight one saves idle workgroups).
+ *                 is laid out and divided for it.  (Give a tight one: where it is 32 times the lengths a call takes several times as long.)
  *   window        0 (none) or the number of last places seen.
  *   workspace     dycl_op_attend_workspace(...) bytes, 16-byte aligned, or NULL when that is 0.
  * Scores, softmax and sums are float32.  The softmax's weights enter the second product as

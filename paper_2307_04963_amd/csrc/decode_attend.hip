@@ -9,7 +9,7 @@
 // that only reads reaches 6.2); 2 rows of 131072, 16 heads on 2 of 256, 537 MB in 92 + 7; one row of 4095 keys,
 // 32 on 8 of 128, 5.7 + 3.6, which is three dependent trips to memory (table, keys and values,
 // results) and a second launch; 37 rows of up to 3001 keys, 16 heads of 64, a window of 2048 and three of ten places
-// closed, 129 MB in 36 + 4: its 5000 workgroups are short, and all their places' scores are looked over.
+// closed, 129 MB in 39 + 4: its 5000 workgroups are short, and all their places' scores are looked over.
 //
 // A tile is 32 keys of one head.  Scores are K Q^T: row i of the first matrix
 // instruction of two is key 8 (i / 4) + i % 4 of the tile, of the second 4 more, so a lane's
@@ -40,7 +40,7 @@ template <int DP>
 struct Shape {
   static constexpr int kTiles = DP <= 64 ? 2 : 1;                  // per wave of a part
   static constexpr int kPart = kWaves * kTiles * kTile;            // keys of a part
-  static constexpr int kRun = 512 / kPart, kStretch = 2048 / kPart;   // parts of each
+  static constexpr int kRun = 512 / kPart;                         // parts of a run
 };
 constexpr int kRunKeys = 512, kStretchKeys = 2048, kFour = 4;
 
@@ -494,10 +494,13 @@ constexpr uint32_t kMaxGrid = 1u << 23;
 int part_keys(int dim) { return dim <= 64 ? Shape<64>::kPart : Shape<128>::kPart; }
 
 // What a workgroup takes, by the stretches that there are (heads of the cache x rows x capacity): a whole one from three per CU on
-// (768 of 128 dims: 146 us, in runs 149, in parts 159; 1024: 188, 195, 210), but from one per CU on if rows are of 16 or
-// more, whose unequal lengths then leave little idle (256 of 256 dims: 95 + 7 us, 106 + 8 in runs); fewer leave CUs idle
-// and each takes 20 to 60 us by itself (64 of 128 dims: 34 us, 17 in runs, 18 in parts).  Runs from one stretch per CU on
-// (384 of 128 dims: 77 us, in parts 83), for 64 dims never (384: 36 and 38, with a mask 33 and 30).
+// (768 of 128 dims: 144 us, in runs 150, in parts 158; 1024: 190, 197, 208), but from one per CU on if rows are of 16 or
+// more, whose unequal lengths then leave little idle (256 of 256 dims: 108 us, 115 in runs); fewer leave CUs idle
+// and each takes 20 to 60 us by itself (64 of 128 dims: 36 us, 17 in runs or parts).  Runs from one stretch per CU on
+// (384 of 128 dims: 79 us, in parts 83), for 64 dims never (384: 47 in parts and 56, with a mask 34 and 38).  Stretches of 64 dims are as
+// fast as parts where lengths are unequal and masked (768: 61 and 62 us), up to 15 % slower where they are equal (1024: 131, 114).
+// The capacity stands for the lengths, which the host does not know: far above them few workgroups have all the work (one row of
+// 4095 keys, 32 heads on 8 of 128: 10 us, with a table for 32768 tokens 15, for 131072 49).
 Parts parts_of(int64_t n, int q_heads, int heads, int dim, int64_t max_length, int64_t window, void* workspace) {
   Parts d;
   const int64_t longest = window ? std::min(max_length, window + kTile - 1) : max_length;

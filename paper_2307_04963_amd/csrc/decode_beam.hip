@@ -8,9 +8,10 @@
 // holds (a row of equal values) the k are taken one after the other.  A second kernel sums a beam's segments, in order, and
 // takes the k largest of the segments' lists the same way.
 //
-// Bound by HBM (a logit is read once) and close behind by instruction issue: about 12 vector
-// instructions per logit, the exponential 4 of them.  Measured: 512 rows of 131072 logits in float32 44 us
-// (6.0 TB/s; 54 behind a reordering whose writes are still on their way), in bf16 38 us (3.5 TB/s: issue);
+// Bound by HBM in float32 (a logit is read once); about 12 vector instructions per logit, the exponential at a quarter of their
+// rate, which is 25 us for 67 million.  Measured: 512 rows of 131072 logits in float32 44 us
+// (6.0 TB/s; 54 behind a reordering whose writes are still on their way), in bf16 38 us (3.5 TB/s), where neither the bytes (25 us)
+// nor the instructions are the bound: a workgroup's requests, its sums and its list follow one another;
 // the second kernel 4 us for one sequence, 6 for 64 of 1024 candidates, 13 for 16 of 12800.
 #include "decode_dev.hpp"
 

@@ -335,8 +335,8 @@ void launch_wide(const RotateArgs& a, const Units& u, dim3 grid, hipStream_t str
 }  // namespace
 
 void decode_rotate(const RotateArgs& a, hipStream_t stream) {
-  // Values of a unit: 16, 8 or 4 bytes, the most that the sizes are multiples of.  (Pairs of which no two lie together in float32,
-  // or four in bf16: the kernel that looks at every unit's length, at a third of the rate.)
+  // Values of a unit: 16, 8 or 4 bytes, the most that the sizes are multiples of.  (An odd number of pairs in halves, or an odd dim or rest: the
+  // kernel that looks at every unit's length, at a third of the rate: 32768 rows of 16 heads of 72 in bf16, 9 pairs 98 us, 18 33.)
   const int rest = a.dim - 2 * a.pairs, most = a.f32 ? kWide<true> : kWide<false>;
   int wide = most;
   while (wide > 1 && ((a.interleaved ? 2 * a.pairs : a.pairs) % wide || rest % wide || a.dim % wide)) wide /= 2;
@@ -348,9 +348,13 @@ void decode_rotate(const RotateArgs& a, hipStream_t stream) {
   const int turned = units(a.interleaved ? 2 * a.pairs : a.pairs, 1), copied = units(rest, vectors);
   const int plain = units(a.dim, vectors), q_heads = a.q ? a.q_heads : 0, heads = a.k ? a.cache.heads : 0;
   const int of_q = q_heads * (turned + copied), of_row = of_q + heads * (turned + copied + plain);
-  // Rows of a tile, fewer where they would not fill the CUs: about two units per lane (16383 rows of 20 heads of 96 in float32:
-  // 41 us with a row of 480 units each, 44 to 50 with 2 to 8), and with a cache more, for each tile waits for its
-  // rows' pages (6000 rows of 48 heads of 128 in bf16: 31 us with a row of 384 units each, 26 with 6 or 8).
+  // Rows of a tile, fewer where they would not fill the CUs: about two units per lane, and with a cache ten, for each tile waits for its
+  // rows' pages.  Measured over rows of 64 to 16384 values, 300 to 32768 of them, both types: 512 units are within 7 % of the best of
+  // 128 to 2048; 128 take up to twice as long where rows are narrow (32768 of 16 heads of 72: 67 us, 33), 2048 17 % more
+  // (8000 of 32 of 128: 31, 27).  With a cache, eight layouts, 300 to 20000 rows: 2560 within 10 % of the best of 256 to 5120; 256 up to
+  // half as much again (20000 of 16 + 2 heads of 128: 64, 41), 5120 17 % more (6000 of 32 + 8 of 128: 37, 32).  Tiles
+  // at least: 4096 instead of 1024 take up to twice as long (8000 rows of 64: 9 us, 4), 256 from 22 % less to 6 % more; with a cache 256
+  // instead of 512 up to 30 % more and 1024 up to half as much again (2000 rows of 16 + 2 heads of 128: 9.9, 7.6, 9.3 us; of 4 + 1 of 64: 4.5, 4.9, 7.3).
   int64_t rows = (whole ? (a.k ? 2560 : 512) * (most / wide) : 1024) / of_row;
   if (a.pairs) rows = std::min<int64_t>(rows, kTableSize / a.pairs);
   rows = std::max<int64_t>(1, std::min<int64_t>({rows, kMaxRows, a.n / (a.k ? 512 : 1024)}));
